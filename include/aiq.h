@@ -51,7 +51,7 @@
 extern "C" {
 #endif
 
-#define AIQ_ABI_VERSION 6
+#define AIQ_ABI_VERSION 7
 
 typedef enum aiq_status {
   AIQ_OK = 0,
@@ -95,6 +95,8 @@ typedef enum aiq_logits_mode { AIQ_LOGITS_LABELS = 1, AIQ_LOGITS_FULL_VOCAB = 2 
                                      the pairs past it are dropped                  */
 #define AIQ_DEV_SCAN_WAIT   0x100 /* a compaction block waited too long for an
                                      earlier block's totals: outputs invalid       */
+#define AIQ_DEV_KV_RANGE 0x200    /* a sequence of a cache batch with a length, rows, tail or
+                                     block number outside its bounds: left out      */
 
 /* indices into aiq_out.scalars (int64, device) */
 #define AIQ_S_SELECTED 0   /* rows passing WHERE (and the join)                      */
@@ -504,6 +506,151 @@ aiq_status aiq_prefill_packed(const aiq_plan* plan, const int32_t* tok, const in
  */
 aiq_status aiq_convert_weights(const void* src, int32_t src_dtype, void* dst, int32_t dst_dtype, int64_t n,
                                void* stream);
+
+/* ------------------------------------------------------------------------
+ * Keys and values in 8 bits: the cache that a generation step of AI_TRANSFORM
+ * (Table 1) writes and attends over, for callers that run steps of their own.
+ *
+ * A sequence's tokens lie in blocks of AIQ_KV_BLOCK.  A full block holds, per
+ * K/V head, its keys and its values as 8-bit whole numbers with one fp32
+ * scale each:
+ *     scale = max(max |x| over the block's tokens and the head's dims, 2^-80) / 127
+ *     q     = x / scale rounded to the nearest whole number (ties to even)
+ * and reads back as q * scale.  A block that holds an infinity or a NaN gets
+ * the scale NaN.  The tokens of a last block that is not full yet stay in 16
+ * bits in the sequence's tail; the block is quantised from those when its
+ * last token arrives.  So what the cache holds is a function of the tokens
+ * alone, however many calls wrote them.
+ *
+ * The arrangement of bytes inside a block is the library's own (the order in
+ * which the attention's matrix instructions take them): blocks and tails may
+ * be copied or moved whole, and are read through aiq_kv_read.
+ */
+#define AIQ_KV_BLOCK 32
+
+typedef struct aiq_kv_cache {
+  void* k;                 /* device, n_blocks * n_kv_heads * AIQ_KV_BLOCK * head_dim bytes */
+  void* v;                 /* ... the values */
+  float* k_scale;          /* device [n_blocks, n_kv_heads] */
+  float* v_scale;
+  void* tail;              /* device [n_tails, 2, n_kv_heads, AIQ_KV_BLOCK, head_dim] of dtype: keys, values */
+  int32_t n_blocks, n_tails;
+  int32_t n_kv_heads;
+  int32_t head_dim;        /* 64 or 128 */
+  int32_t dtype;           /* AIQ_F16 or AIQ_BF16: keys, values, queries and the tail */
+  int32_t reserved;
+} aiq_kv_cache;
+
+/*
+ * The sequences of a call.  Sequence i holds len[i] tokens once the call's
+ * own are in; the call's rows cu[i] .. cu[i+1] are its last cu[i+1] - cu[i]
+ * tokens (cu NULL: row i is the last token of sequence i; an empty slot has
+ * len[i] = 0).  Its blocks are entries blk_start[i] .. blk_start[i+1] of
+ * blk_ids (blk_ids NULL: entry e is block e), its tail is tail_ids[i] (NULL:
+ * i).  Sequences may share full blocks (a common prompt); a block or a tail
+ * that a call writes belongs to one sequence alone.  Rows past the last
+ * sequence's are not touched.
+ * A sequence whose numbers do not fit (len[i] above max_len or its blocks, more
+ * rows than tokens, a tail or block number out of range) sets
+ * AIQ_DEV_KV_RANGE in *status, and nothing of it is read or written out of
+ * bounds; its outputs are unspecified.
+ */
+typedef struct aiq_kv_batch {
+  int32_t n_seq;
+  int32_t max_len;           /* host: bound on len[i]; sizes the split of long sequences */
+  int64_t n_rows;            /* host: rows of the call (n_seq where cu is NULL) */
+  const int32_t* len;        /* device [n_seq] */
+  const int32_t* cu;         /* device [n_seq + 1], or NULL */
+  const int32_t* blk_start;  /* device [n_seq + 1] */
+  const int32_t* blk_ids;    /* device, or NULL */
+  const int32_t* tail_ids;   /* device [n_seq], or NULL */
+  int64_t* status;           /* device word that AIQ_DEV_KV_RANGE is set in, or NULL */
+} aiq_kv_batch;
+
+/*
+ * Writes the call's rows into the cache (Table 1's AI_TRANSFORM: the keys and
+ * values that later positions read).  k and v: device rows of n_kv_heads *
+ * head_dim elements of the cache's dtype, k_ld and v_ld elements apart (so
+ * they may be columns of q|k|v rows); 16-byte aligned, the strides multiples
+ * of 8.  Appending must be in order: the earlier len[i] - n tokens of
+ * a sequence are in the cache.  Writing a row again has the same result as
+ * long as no later block has been begun.
+ * Errors: AIQ_EINVAL (NULL pointer, negative count, head_dim, stride or
+ * alignment, cu NULL with n_rows != n_seq), AIQ_EUNSUPPORTED (dtype),
+ * AIQ_EHIP.  Nothing is enqueued for an empty batch.
+ */
+aiq_status aiq_kv_write(const aiq_kv_cache* cache, const aiq_kv_batch* batch, const void* k, int64_t k_ld,
+                        const void* v, int64_t v_ld, void* stream);
+
+/*
+ * Reads the batch's rows back: row cu[i] + t receives token len[i] - n + t of
+ * sequence i, n = cu[i+1] - cu[i], in the cache's dtype (8-bit values times
+ * their scale, rounded once; tail tokens as they were written).  k_out and
+ * v_out as aiq_kv_write's k and v.  Errors: as aiq_kv_write.
+ */
+aiq_status aiq_kv_read(const aiq_kv_cache* cache, const aiq_kv_batch* batch, void* k_out, int64_t k_ld, void* v_out,
+                       int64_t v_ld, void* stream);
+
+/* Bytes of workspace aiq_kv_attend needs for a batch of these counts (n_seq, n_rows, max_len,
+ * whether cu is NULL); 0 where no sequence's keys are split between workgroups.
+ * Table 1's AI_TRANSFORM.  Errors: as aiq_kv_attend. */
+aiq_status aiq_kv_attend_workspace_size(const aiq_kv_cache* cache, const aiq_kv_batch* batch, int32_t n_heads,
+                                        size_t* bytes);
+
+/*
+ * Attention of the batch's rows over the cache (Table 1's AI_TRANSFORM): row
+ * cu[i] + t is the query at position p = len[i] - n + t of sequence i and sees
+ * the tokens 0 .. p, which are in the cache (its own included);
+ *     out = sum_j softmax_j(q . k_j / sqrt(head_dim)) v_j
+ * with query head h reading K/V head h / (n_heads / n_kv_heads).  q: rows of
+ * n_heads * head_dim elements of the cache's dtype, q_ld apart; out: the same
+ * in out_dtype (AIQ_F16 or AIQ_BF16), out_ld apart; aligned as aiq_kv_write's
+ * rows.  The row of an empty slot (len[i] = 0) becomes zero.  A query sees a
+ * token only through the scale of its block: an infinity or NaN in the block
+ * of a visible token reaches the output, one in later blocks does not.  With
+ * one row per sequence the result does not depend on the other sequences.
+ * workspace: 256-byte aligned, aiq_kv_attend_workspace_size bytes (NULL where
+ * that is 0); calls that may overlap need one each.  Errors: AIQ_EINVAL (as
+ * aiq_kv_write; n_heads not a multiple of n_kv_heads), AIQ_EUNSUPPORTED
+ * (dtype), AIQ_ENOSPC (ws_bytes), AIQ_EHIP.
+ */
+aiq_status aiq_kv_attend(const aiq_kv_cache* cache, const aiq_kv_batch* batch, const void* q, int64_t q_ld,
+                         int32_t n_heads, void* out, int64_t out_ld, int32_t out_dtype, void* workspace,
+                         size_t ws_bytes, void* stream);
+
+/*
+ * The next token of each row of logits (Table 1's AI_TRANSFORM, decoding by
+ * sampling): row r is logits[r * ld .. r * ld + vocab) in dtype (AIQ_F32,
+ * AIQ_F16 or AIQ_BF16; ld 0: the same row for every r).  With m the row's maximum, token i weighs
+ *     w_i = exp((x_i - m) / temperature)
+ * and the tokens ordered by logit, descending, equal ones by id, ascending,
+ * are cut to their first n = min(n_k, n_p, n_m):
+ *     n_k = top_k (0: the vocabulary)
+ *     n_p = the fewest whose weights reach top_p of the first n_k's sum
+ *     n_m = those with w_i >= min_p
+ * The row's token is the lowest id i of the kept for which the kept weights of
+ * the ids up to i sum to more than u[r] times all of theirs.  u: device [n_rows] numbers in
+ * [0, 1), the caller's random numbers (one above or NaN takes the last kept id).
+ * temperature 0 takes the maximum's lowest id (u may be NULL).  NaN and
+ * -infinity are never taken, unless the row holds nothing else (token 0);
+ * where the maximum is +infinity, its tokens weigh 1 and the others nothing.
+ * Weights are taken from fp64 exponentials and summed as whole numbers, so
+ * results do not depend on an order of summation.
+ * vocab at most 2^24, ld >= vocab or 0.  Errors: AIQ_EINVAL (NULL pointer,
+ * negative count or top_k, temperature negative or not finite, top_p
+ * outside (0, 1], min_p outside [0, 1], logits not aligned to their type),
+ * AIQ_EUNSUPPORTED (dtype), AIQ_EHIP.
+ */
+typedef struct aiq_sampling {
+  double temperature;
+  double top_p;              /* 1 = off */
+  double min_p;              /* 0 = off */
+  int32_t top_k;             /* 0 = off */
+  int32_t reserved;
+} aiq_sampling;
+
+aiq_status aiq_sample(const void* logits, int32_t dtype, int64_t ld, int32_t vocab, int64_t n_rows,
+                      const aiq_sampling* sampling, const float* u, int32_t* token, void* stream);
 
 /* Frees a plan (host memory only; NULL is ignored). */
 void aiq_plan_destroy(aiq_plan* plan);

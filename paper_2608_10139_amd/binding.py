@@ -13,7 +13,7 @@ import os
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libaiq.so")
 
-AIQ_ABI_VERSION = 6   # the struct layouts below
+AIQ_ABI_VERSION = 7   # the struct layouts below
 AIQ_OK, AIQ_EINVAL, AIQ_EUNSUPPORTED, AIQ_ENOSPC, AIQ_EHIP, AIQ_ENOMEM = 0, -1, -2, -3, -4, -5
 AIQ_I8, AIQ_I16, AIQ_I32, AIQ_F32, AIQ_BF16, AIQ_F16 = 1, 2, 3, 4, 5, 6
 AIQ_LT, AIQ_LE, AIQ_GT, AIQ_GE, AIQ_EQ, AIQ_NE, AIQ_IN = range(7)
@@ -28,11 +28,12 @@ AIQ_PLAN_FULL_LAST_LAYER = 8
 
 AIQ_DEV_TOKEN_RANGE, AIQ_DEV_DUP_KEY, AIQ_DEV_HASH_FULL, AIQ_DEV_IDS_CAP = 0x01, 0x02, 0x04, 0x08
 AIQ_DEV_GROUP_RANGE, AIQ_DEV_LIST_LEN, AIQ_DEV_GROUP_CAP, AIQ_DEV_PAIR_CAP = 0x10, 0x20, 0x40, 0x80
-AIQ_DEV_SCAN_WAIT = 0x100
+AIQ_DEV_SCAN_WAIT, AIQ_DEV_KV_RANGE = 0x100, 0x200
 AIQ_S_SELECTED, AIQ_S_KEPT, AIQ_S_TOKENS, AIQ_S_STATUS, AIQ_S_GROUPS, AIQ_S_PAIRS = range(6)
 AIQ_N_SCALARS = 8
 AIQ_MAX_PREDS, AIQ_MAX_IN_SET, AIQ_MAX_PREFIX, AIQ_MAX_LABELS = 8, 32, 64, 8
 AIQ_MAX_GEN, AIQ_MAX_LIKE = 512, 16
+AIQ_KV_BLOCK = 32
 
 (AIQ_K_REL, AIQ_K_PACK, AIQ_K_EMBED, AIQ_K_NORM, AIQ_K_GEMM_QKV, AIQ_K_ATTN, AIQ_K_GEMM_O,
  AIQ_K_GEMM_UP, AIQ_K_GEMM_DOWN, AIQ_K_HEAD, AIQ_K_AGG, AIQ_K_DECODE, AIQ_K_DECODE_ATTN,
@@ -101,10 +102,28 @@ class aiq_trace(C.Structure):
                 ("capacity", C.c_int32), ("count", C.c_int32), ("kind_mask", C.c_uint32)]
 
 
+class aiq_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("tail", C.c_void_p), ("n_blocks", C.c_int32), ("n_tails", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class aiq_kv_batch(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("max_len", C.c_int32), ("n_rows", C.c_int64), ("len", C.c_void_p),
+                ("cu", C.c_void_p), ("blk_start", C.c_void_p), ("blk_ids", C.c_void_p), ("tail_ids", C.c_void_p),
+                ("status", C.c_void_p)]
+
+
+class aiq_sampling(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 EXPORTS = ("aiq_plan_create", "aiq_workspace_size", "aiq_plan_passes", "aiq_plan_chunk_tokens",
            "aiq_plan_last_layer_rows", "aiq_run", "aiq_run_relational_static", "aiq_convert_weights",
            "aiq_prefill_workspace_size",
-           "aiq_prefill_packed", "aiq_plan_destroy", "aiq_status_str", "aiq_abi_version")
+           "aiq_prefill_packed", "aiq_kv_write", "aiq_kv_read", "aiq_kv_attend_workspace_size", "aiq_kv_attend",
+           "aiq_sample", "aiq_plan_destroy", "aiq_status_str", "aiq_abi_version")
 
 
 class AiqError(RuntimeError):
@@ -146,6 +165,17 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     lib.aiq_prefill_workspace_size.restype = C.c_int
     lib.aiq_prefill_packed.argtypes = [P, P, P, C.c_int32, C.c_int64, C.c_int32, P, P, C.c_size_t, P]
     lib.aiq_prefill_packed.restype = C.c_int
+    KV, KB = C.POINTER(aiq_kv_cache), C.POINTER(aiq_kv_batch)
+    lib.aiq_kv_write.argtypes = [KV, KB, P, C.c_int64, P, C.c_int64, P]
+    lib.aiq_kv_write.restype = C.c_int
+    lib.aiq_kv_read.argtypes = [KV, KB, P, C.c_int64, P, C.c_int64, P]
+    lib.aiq_kv_read.restype = C.c_int
+    lib.aiq_kv_attend_workspace_size.argtypes = [KV, KB, C.c_int32, C.POINTER(C.c_size_t)]
+    lib.aiq_kv_attend_workspace_size.restype = C.c_int
+    lib.aiq_kv_attend.argtypes = [KV, KB, P, C.c_int64, C.c_int32, P, C.c_int64, C.c_int32, P, C.c_size_t, P]
+    lib.aiq_kv_attend.restype = C.c_int
+    lib.aiq_sample.argtypes = [P, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.POINTER(aiq_sampling), P, P, P]
+    lib.aiq_sample.restype = C.c_int
     lib.aiq_plan_destroy.argtypes = [P]
     lib.aiq_plan_destroy.restype = None
     lib.aiq_status_str.argtypes = [C.c_int32]
@@ -245,6 +275,33 @@ def aiq_prefill_packed(plan, tok_ptr: int, cu_ptr: int, n_seq: int, n_tok: int, 
                        logits_ptr: int, ws_ptr: int, ws_bytes: int, stream: int = 0) -> None:
     check("aiq_prefill_packed", load().aiq_prefill_packed(plan, tok_ptr, cu_ptr, n_seq, n_tok, mode,
                                                           logits_ptr, ws_ptr, ws_bytes, stream))
+
+
+def aiq_kv_write(cache, batch, k_ptr: int, k_ld: int, v_ptr: int, v_ld: int, stream: int = 0) -> None:
+    check("aiq_kv_write", load().aiq_kv_write(C.byref(cache), C.byref(batch), k_ptr, k_ld, v_ptr, v_ld, stream))
+
+
+def aiq_kv_read(cache, batch, k_ptr: int, k_ld: int, v_ptr: int, v_ld: int, stream: int = 0) -> None:
+    check("aiq_kv_read", load().aiq_kv_read(C.byref(cache), C.byref(batch), k_ptr, k_ld, v_ptr, v_ld, stream))
+
+
+def aiq_kv_attend_workspace_size(cache, batch, n_heads: int) -> int:
+    n = C.c_size_t()
+    check("aiq_kv_attend_workspace_size",
+          load().aiq_kv_attend_workspace_size(C.byref(cache), C.byref(batch), n_heads, C.byref(n)))
+    return n.value
+
+
+def aiq_kv_attend(cache, batch, q_ptr: int, q_ld: int, n_heads: int, out_ptr: int, out_ld: int, out_dtype: int,
+                  ws_ptr: int, ws_bytes: int, stream: int = 0) -> None:
+    check("aiq_kv_attend", load().aiq_kv_attend(C.byref(cache), C.byref(batch), q_ptr, q_ld, n_heads, out_ptr, out_ld,
+                                                out_dtype, ws_ptr, ws_bytes, stream))
+
+
+def aiq_sample(logits_ptr: int, dtype: int, ld: int, vocab: int, n_rows: int, sampling: aiq_sampling, u_ptr: int,
+               token_ptr: int, stream: int = 0) -> None:
+    check("aiq_sample", load().aiq_sample(logits_ptr, dtype, ld, vocab, n_rows, C.byref(sampling), u_ptr, token_ptr,
+                                          stream))
 
 
 def aiq_plan_destroy(plan) -> None:

@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -1359,6 +1360,138 @@ aiq_status aiq_convert_weights(const void* src, int32_t src_dtype, void* dst, in
   if (src_dtype != AIQ_BF16 || dst_dtype != AIQ_F16) return AIQ_EUNSUPPORTED;
   if (reinterpret_cast<uintptr_t>(src) % 16 || reinterpret_cast<uintptr_t>(dst) % 16) return AIQ_EINVAL;
   HIP_TRY(launch_bf16_to_f16(src, dst, n, static_cast<hipStream_t>(stream)));
+  return AIQ_OK;
+}
+
+// The cache and batch of a call as the kernels take them, or why not.
+namespace {
+
+aiq_status kv_args(const aiq_kv_cache* c, const aiq_kv_batch* b, KvCache* kc, KvBatch* kb) {
+  if (!c || !b) return AIQ_EINVAL;
+  if (c->dtype != AIQ_F16 && c->dtype != AIQ_BF16) return AIQ_EUNSUPPORTED;
+  if (c->n_blocks < 0 || c->n_tails < 0 || c->n_kv_heads <= 0 || (c->head_dim != 64 && c->head_dim != 128))
+    return AIQ_EINVAL;
+  if (c->n_blocks > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return AIQ_EINVAL;
+  if (c->n_tails > 0 && !c->tail) return AIQ_EINVAL;
+  for (const void* p : {c->k, c->v, c->tail})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return AIQ_EINVAL;
+  if (reinterpret_cast<uintptr_t>(c->k_scale) % 4 || reinterpret_cast<uintptr_t>(c->v_scale) % 4) return AIQ_EINVAL;
+  if (b->n_seq < 0 || b->n_rows < 0 || b->n_rows > INT32_MAX || b->max_len < 0) return AIQ_EINVAL;
+  if (b->n_seq > 0 && (!b->len || !b->blk_start)) return AIQ_EINVAL;
+  if (!b->cu && b->n_rows != b->n_seq) return AIQ_EINVAL;
+  if (reinterpret_cast<uintptr_t>(b->status) % 8) return AIQ_EINVAL;
+  kc->k = static_cast<uint8_t*>(c->k);
+  kc->v = static_cast<uint8_t*>(c->v);
+  kc->ks = c->k_scale;
+  kc->vs = c->v_scale;
+  kc->tail = static_cast<uint16_t*>(c->tail);
+  kc->n_blocks = c->n_blocks;
+  kc->n_tails = c->n_tails;
+  kc->n_kv = c->n_kv_heads;
+  kc->hd = c->head_dim;
+  kc->act = c->dtype == AIQ_F16 ? 2 : 1;
+  *kb = KvBatch{};
+  kb->n_seq = b->n_seq;
+  kb->max_len = b->max_len;
+  kb->n_rows = b->n_rows;
+  kb->len = b->len;
+  kb->cu = b->cu;
+  kb->blk_start = b->blk_start;
+  kb->blk_ids = b->blk_ids;
+  kb->tail_ids = b->tail_ids;
+  kb->status = b->status;
+  return AIQ_OK;
+}
+
+// rows of `width` 16-bit elements, ld apart, read in 16-byte pieces
+bool kv_rows_ok(const void* p, int64_t ld, int64_t width) {
+  return p && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld >= width && ld % 8 == 0;
+}
+
+aiq_status kv_move(const aiq_kv_cache* cache, const aiq_kv_batch* batch, const void* k, int64_t k_ld, const void* v,
+                   int64_t v_ld, bool write, void* stream) {
+  KvCache c;
+  KvBatch b;
+  const aiq_status e = kv_args(cache, batch, &c, &b);
+  if (e != AIQ_OK) return e;
+  const int64_t width = static_cast<int64_t>(c.n_kv) * c.hd;
+  if (b.n_rows > 0 && (!kv_rows_ok(k, k_ld, width) || !kv_rows_ok(v, v_ld, width))) return AIQ_EINVAL;
+  const KvRows r{static_cast<uint16_t*>(const_cast<void*>(k)), static_cast<uint16_t*>(const_cast<void*>(v)), k_ld, v_ld};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  HIP_TRY(write ? launch_kv_write(c, b, r, s) : launch_kv_read(c, b, r, s));
+  return AIQ_OK;
+}
+
+}  // namespace
+
+aiq_status aiq_kv_write(const aiq_kv_cache* cache, const aiq_kv_batch* batch, const void* k, int64_t k_ld,
+                        const void* v, int64_t v_ld, void* stream) {
+  return kv_move(cache, batch, k, k_ld, v, v_ld, true, stream);
+}
+
+aiq_status aiq_kv_read(const aiq_kv_cache* cache, const aiq_kv_batch* batch, void* k_out, int64_t k_ld, void* v_out,
+                       int64_t v_ld, void* stream) {
+  return kv_move(cache, batch, k_out, k_ld, v_out, v_ld, false, stream);
+}
+
+aiq_status aiq_kv_attend_workspace_size(const aiq_kv_cache* cache, const aiq_kv_batch* batch, int32_t n_heads,
+                                        size_t* bytes) {
+  KvCache c;
+  KvBatch b;
+  const aiq_status e = kv_args(cache, batch, &c, &b);
+  if (e != AIQ_OK) return e;
+  if (!bytes || n_heads <= 0 || n_heads % c.n_kv) return AIQ_EINVAL;
+  *bytes = kv_attend_part_bytes(c, b, n_heads);
+  return AIQ_OK;
+}
+
+aiq_status aiq_kv_attend(const aiq_kv_cache* cache, const aiq_kv_batch* batch, const void* q, int64_t q_ld,
+                         int32_t n_heads, void* out, int64_t out_ld, int32_t out_dtype, void* workspace,
+                         size_t ws_bytes, void* stream) {
+  KvAttendArgs a{};
+  const aiq_status e = kv_args(cache, batch, &a.c, &a.b);
+  if (e != AIQ_OK) return e;
+  if (n_heads <= 0 || n_heads % a.c.n_kv) return AIQ_EINVAL;
+  if (out_dtype != AIQ_F16 && out_dtype != AIQ_BF16) return AIQ_EUNSUPPORTED;
+  const int64_t width = static_cast<int64_t>(n_heads) * a.c.hd;
+  if (a.b.n_rows > 0 && (!kv_rows_ok(q, q_ld, width) || !kv_rows_ok(out, out_ld, width))) return AIQ_EINVAL;
+  const size_t need = kv_attend_part_bytes(a.c, a.b, n_heads);
+  if (need > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % ALIGN)) return AIQ_EINVAL;
+  if (ws_bytes < need) return AIQ_ENOSPC;
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_ld = q_ld;
+  a.n_heads = n_heads;
+  a.out = static_cast<uint16_t*>(out);
+  a.out_ld = out_ld;
+  a.out_act = out_dtype == AIQ_F16 ? 2 : 1;
+  a.part = need > 0 ? static_cast<float*>(workspace) : nullptr;
+  HIP_TRY(launch_kv_attend(a, static_cast<hipStream_t>(stream)));
+  return AIQ_OK;
+}
+
+aiq_status aiq_sample(const void* logits, int32_t dtype, int64_t ld, int32_t vocab, int64_t n_rows,
+                      const aiq_sampling* sm, const float* u, int32_t* token, void* stream) {
+  if (!sm || n_rows < 0 || vocab <= 0 || vocab > (1 << 24) || (ld < vocab && ld != 0)) return AIQ_EINVAL;
+  if (dtype != AIQ_F32 && dtype != AIQ_F16 && dtype != AIQ_BF16) return AIQ_EUNSUPPORTED;
+  if (!(sm->temperature >= 0.0) || !std::isfinite(sm->temperature) || !(sm->top_p > 0.0) || !(sm->top_p <= 1.0) ||
+      !(sm->min_p >= 0.0) || !(sm->min_p <= 1.0) || sm->top_k < 0)
+    return AIQ_EINVAL;
+  if (n_rows == 0) return AIQ_OK;
+  if (!logits || !token || (sm->temperature > 0.0 && !u)) return AIQ_EINVAL;
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == AIQ_F32 ? 4 : 2)) return AIQ_EINVAL;
+  SampleArgs a{};
+  a.logits = logits;
+  a.dtype = dtype;
+  a.ld = ld;
+  a.vocab = vocab;
+  a.n_rows = n_rows;
+  a.temperature = sm->temperature;
+  a.top_p = sm->top_p;
+  a.min_p = sm->min_p;
+  a.top_k = sm->top_k >= vocab ? 0 : sm->top_k;
+  a.u = u;
+  a.token = token;
+  HIP_TRY(launch_sample(a, static_cast<hipStream_t>(stream)));
   return AIQ_OK;
 }
 

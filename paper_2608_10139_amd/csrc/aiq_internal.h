@@ -488,6 +488,68 @@ hipError_t launch_gen_like(const int32_t* gen, const int64_t* n_ptr, int64_t n_u
 hipError_t launch_copy_rows_i32(const int32_t* src, const int64_t* n_ptr, int64_t n_ub, int32_t per_row,
                                 int32_t* dst, int64_t cap_rows, hipStream_t s);
 
+// ---------------------------------------------------------------- 8-bit key/value cache
+// aiq_kv_cache and aiq_kv_batch as the kernels take them.  Beyond the public
+// batch: the number of sequences from device memory (n_ptr, else n_seq, which
+// bounds it) and len[i] + len_add for the length.
+struct KvCache {
+  uint8_t* k;
+  uint8_t* v;
+  float* ks;
+  float* vs;
+  uint16_t* tail;
+  int32_t n_blocks, n_tails, n_kv, hd, act;   // act: ACT_F16 or ACT_BF16
+};
+struct KvBatch {
+  int32_t n_seq, max_len;
+  int64_t n_rows;
+  const int64_t* n_ptr;
+  const int32_t* len;
+  int32_t len_add;
+  const int32_t* cu;
+  const int32_t* blk_start;
+  const int32_t* blk_ids;
+  const int32_t* tail_ids;
+  int64_t* status;
+};
+// Rows of keys and values: k + r * k_ld and v + r * v_ld.
+struct KvRows {
+  uint16_t* k;
+  uint16_t* v;
+  int64_t k_ld, v_ld;
+};
+hipError_t launch_kv_write(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t s);
+hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t s);
+struct KvAttendArgs {
+  KvCache c;
+  KvBatch b;
+  const uint16_t* q;
+  int64_t q_ld;
+  int32_t n_heads;
+  uint16_t* out;
+  int64_t out_ld;
+  int32_t out_act;
+  float* part;               // partial results of split sequences (kv_attend_part_bytes), or null
+};
+size_t kv_attend_part_bytes(const KvCache& c, const KvBatch& b, int32_t n_heads);
+hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- sampling
+struct SampleArgs {
+  const void* logits;
+  int32_t dtype;             // AIQ_F32, AIQ_F16 or AIQ_BF16
+  int64_t ld;
+  int32_t vocab;
+  int64_t n_rows;            // host bound
+  const int64_t* n_ptr;      // device: number of rows, or null
+  double temperature;        // 0: the maximum
+  double top_p, min_p;
+  int32_t top_k;             // 0: off
+  const float* u;
+  int32_t* token;
+};
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+
 // Fixed device scratch of the entry point that allocates nothing
 // (aiq_run_relational_static): STATIC_SCRATCH_BYTES of device memory per GPU,
 // held until the process ends.  Returns its device address on the current

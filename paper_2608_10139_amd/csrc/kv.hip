@@ -1,0 +1,870 @@
+// Keys and values in 8 bits (Table 1's AI_TRANSFORM: the cache that a
+// generation step writes and reads): quantising rows as they are written,
+// reading them back, and attention over the cache.
+//
+// A block holds 32 tokens; per K/V head its keys and its values are bytes
+// u = q + 128 with one fp32 scale each.  Inside a block the bytes lie in the
+// order in which the attention's matrix instructions take them, so that a wave
+// reads a block in whole 1 KB loads, 16 bytes per lane:
+//   keys    token t, dim d: tile t / 16, 64-dim slice d / 64; lane (d % 64 / 16) * 16 + t % 16,
+//           byte d % 16.  S^T = K Q^T on v_mfma_f32_16x16x32_f16 takes 8 dims of a lane per step.
+//   values  token t, dim d: pair of 16-dim tiles d / 32; lane (t % 16 / 4) * 16 + d % 16,
+//           byte (d % 32 / 16) * 8 + (t / 16) * 4 + t % 4.  S^T leaves, per lane, the scores of
+//           4 tokens of each 16-token tile of one query: with the values' tokens in the same
+//           order the weights are the operand of O^T = V^T P^T as they stand.
+// The tail (16 bits) is plain rows.
+#include "aiq_internal.h"
+#include "dev_util.h"
+
+namespace aiq {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+typedef __attribute__((address_space(3))) uint16_t lds_u16;
+
+constexpr int KVB = AIQ_KV_BLOCK;
+
+// ------------------------------------------------------------------ sequences of a batch
+struct KvSeq {
+  int len, n;       // tokens in the cache, the call's rows among them
+  int64_t row0;     // first row of the call
+  int bs;           // first entry of its blocks
+  int tail;
+};
+
+__device__ __forceinline__ void kv_flag(const KvBatch& b) {
+  if (b.status) atomicOr(reinterpret_cast<unsigned long long*>(b.status), static_cast<unsigned long long>(AIQ_DEV_KV_RANGE));
+}
+
+// Sequence i, or false where it is left out (its numbers do not fit, flagged; or it has no rows in this call).
+__device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, int i, KvSeq& s) {
+  s.len = b.len[i] + b.len_add;
+  if (b.cu) {
+    const int c0 = b.cu[i], c1 = b.cu[i + 1];
+    s.row0 = c0;
+    s.n = c1 - c0;
+    if (c0 < 0 || c1 < c0 || c1 > b.n_rows) {
+      kv_flag(b);
+      return false;
+    }
+  } else {
+    s.row0 = i;
+    s.n = s.len == 0 ? 0 : 1;
+  }
+  if (s.n == 0) return false;
+  const int64_t e0 = b.blk_start[i], e1 = b.blk_start[i + 1];
+  s.bs = static_cast<int>(e0);
+  s.tail = b.tail_ids ? b.tail_ids[i] : i;
+  const bool uses_tail = s.len % KVB != 0 || (s.len - s.n) % KVB != 0;
+  if (s.len < s.n || s.len > b.max_len || e0 < 0 || (e1 - e0) * KVB < s.len ||
+      (uses_tail && (s.tail < 0 || s.tail >= c.n_tails))) {
+    kv_flag(b);
+    return false;
+  }
+  return true;
+}
+
+// Block number of entry e, or -1 (flagged) where it is outside the cache.
+__device__ __forceinline__ int kv_block(const KvCache& c, const KvBatch& b, int e) {
+  const int id = b.blk_ids ? b.blk_ids[e] : e;
+  if (id >= 0 && id < c.n_blocks) return id;
+  kv_flag(b);
+  return -1;
+}
+
+__device__ __forceinline__ int kv_count(const KvBatch& b) {
+  if (!b.n_ptr) return b.n_seq;
+  const int64_t n = *b.n_ptr;
+  return n < b.n_seq ? static_cast<int>(n) : b.n_seq;
+}
+
+// Batches with several rows per sequence: sequence i owns the work units from
+// first(i) = per * cu[i] / R + extra * i on, enough for `extra` + its rows / R
+// units; which of them it fills the unit finds out itself.
+__device__ __forceinline__ int64_t unit_first(const KvBatch& b, int i, int per, int R, int extra) {
+  const int64_t c = b.cu[i] < 0 ? 0 : b.cu[i];
+  return c * per / R + static_cast<int64_t>(extra) * i;
+}
+__device__ __forceinline__ int unit_seq(const KvBatch& b, int n, int64_t u, int per, int R, int extra) {
+  int lo = 0, hi = n;   // the last i with first(i) <= u
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (unit_first(b, mid, per, R, extra) <= u)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// ------------------------------------------------------------------ write and read
+// A wave per (32-token block of a sequence that the call touches, K/V head);
+// heads of a block are neighbours, so rows are read whole between them.
+// Bound: HBM (2 bytes per element in, 1 out for full blocks; 2 out for the tail).
+// The wave of a sequence's first touched block reads what the tail holds of
+// it, and then writes the new tail: no other wave touches the tail.
+
+// 4 values of one token as loaded: |x| as 16-bit patterns order like the values (infinity and NaN above all)
+__device__ __forceinline__ uint32_t abs_max(uint32_t m, uint32_t two) {
+  const uint32_t a = two & 0x7FFF7FFFu;
+  const uint32_t lo = (a & 0xFFFFu) > (m & 0xFFFFu) ? (a & 0xFFFFu) : (m & 0xFFFFu);
+  const uint32_t hi = (a >> 16) > (m >> 16) ? (a >> 16) : (m >> 16);
+  return lo | (hi << 16);
+}
+
+// the block's scale and the nearest fp32 of 1 / scale
+__device__ __forceinline__ float block_scale(uint32_t m, int act, float& inv) {
+  uint32_t x = (m & 0xFFFFu) > (m >> 16) ? (m & 0xFFFFu) : (m >> 16);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint32_t y = __shfl_xor(x, o);
+    x = y > x ? y : x;
+  }
+  const uint32_t inf = act == ACT_F16 ? 0x7C00u : 0x7F80u;
+  if (x >= inf) {
+    inv = 0.f;
+    return __uint_as_float(0x7FC00000u);
+  }
+  const float s = fmaxf(act2f(static_cast<uint16_t>(x), act), 0x1p-80f) / 127.0f;
+  inv = 1.0f / s;
+  return s;
+}
+
+// x / scale correctly rounded (quotient, exact remainder, one correction), rounded to a whole
+// number by the add, in the low byte with 128 added.
+__device__ __forceinline__ uint32_t quant(float x, float s, float inv) {
+  const float q = x * inv;
+  const float y = fmaf(fmaf(-q, s, x), inv, q);
+  return __float_as_uint(y + (12582912.0f + 128.0f));   // 1.5 * 2^23
+}
+__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return (a & 0xFFu) | ((b & 0xFFu) << 8) | ((c & 0xFFu) << 16) | (d << 24);
+}
+
+struct KvMoveArgs {
+  KvCache c;
+  KvBatch b;
+  KvRows r;
+};
+
+// entry of the tail: keys (0) or values (1) of K/V head h
+__device__ __forceinline__ uint16_t* tail_at(const KvCache& c, int tail, int kv, int h) {
+  return c.tail + ((static_cast<int64_t>(tail) * 2 + kv) * c.n_kv + h) * (KVB * c.hd);
+}
+
+// work units of a batch: blocks that its rows touch (bound on the host, at most that on the device)
+static __host__ __device__ int64_t move_units(const KvBatch& b) {
+  return b.cu ? b.n_rows / KVB + 2 * static_cast<int64_t>(b.n_seq) : b.n_seq;
+}
+__device__ __forceinline__ int64_t move_count(const KvBatch& b, int n) {
+  const int64_t u = b.cu ? unit_first(b, n, 1, KVB, 2) : n, ub = move_units(b);
+  return u < ub ? u : ub;
+}
+
+// The unit's sequence and block; false: nothing to do.
+__device__ __forceinline__ bool move_unit(const KvCache& c, const KvBatch& b, int n, int64_t u, KvSeq& s, int& jj) {
+  int i = static_cast<int>(u);
+  jj = 0;
+  if (b.cu) {
+    i = unit_seq(b, n, u, 1, KVB, 2);
+    jj = static_cast<int>(u - unit_first(b, i, 1, KVB, 2));
+  }
+  return kv_seq(c, b, i, s);
+}
+
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
+  constexpr int KC = HD / 64;
+  const KvCache& c = a.c;
+  const int n = kv_count(a.b);
+  if (n <= 0) return;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+  const int64_t units = move_count(a.b, n);
+  const int64_t wave = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 6;
+  const int64_t n_waves = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 6;
+  for (int64_t item = wave; item < units * c.n_kv; item += n_waves) {
+    const int64_t u = item / c.n_kv;
+    const int h = static_cast<int>(item - u * c.n_kv);
+    KvSeq s;
+    int jj;
+    if (!move_unit(c, a.b, n, u, s, jj)) continue;
+    const int before = s.len - s.n;
+    const int j = before / KVB + jj;
+    if (j * KVB >= s.len) continue;
+    const uint16_t* kn = a.r.k + s.row0 * a.r.k_ld + h * HD;   // row of token `before`
+    const uint16_t* vn = a.r.v + s.row0 * a.r.v_ld + h * HD;
+    uint16_t* tk = tail_at(c, s.tail, 0, h);
+    uint16_t* tv = tail_at(c, s.tail, 1, h);
+    auto src = [&](const uint16_t* rows, int64_t ld, const uint16_t* tail, int t) {   // token t of block j
+      const int p = j * KVB + t;
+      return p < before ? tail + t * HD : rows + static_cast<int64_t>(p - before) * ld;
+    };
+    if ((j + 1) * KVB <= s.len) {
+      const int id = kv_block(c, a.b, s.bs + j);
+      if (id >= 0) {
+        const int64_t at = static_cast<int64_t>(id) * c.n_kv + h;
+        uint4 kr[2 * KC][2];
+        uint32_t m = 0;
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+          const uint16_t* p = src(kn, a.r.k_ld, tk, tt * 16 + c16) + g * 16;
+#pragma unroll
+          for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) kr[tt * KC + kc][e] = *reinterpret_cast<const uint4*>(p + kc * 64 + e * 8);
+        }
+        uint2 vr[KC][2][4];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint16_t* p = src(vn, a.r.v_ld, tv, tt * 16 + g * 4 + r) + c16 * 4;
+#pragma unroll
+            for (int kc = 0; kc < KC; ++kc) vr[kc][tt][r] = *reinterpret_cast<const uint2*>(p + kc * 64);
+          }
+#pragma unroll
+        for (int i = 0; i < 2 * KC; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            m = abs_max(abs_max(abs_max(abs_max(m, kr[i][e].x), kr[i][e].y), kr[i][e].z), kr[i][e].w);
+        float inv;
+        float sc = block_scale(m, c.act, inv);
+        if (lane == 0) c.ks[at] = sc;
+        uint8_t* kb = c.k + at * (KVB * HD);
+#pragma unroll
+        for (int i = 0; i < 2 * KC; ++i) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t x[4] = {kr[i][e].x, kr[i][e].y, kr[i][e].z, kr[i][e].w};
+            uint32_t b[8];
+#pragma unroll
+            for (int z = 0; z < 8; ++z)
+              b[z] = quant(act2f(static_cast<uint16_t>(z & 1 ? x[z / 2] >> 16 : x[z / 2] & 0xFFFFu), c.act), sc, inv);
+            w[e * 2] = pack4(b[0], b[1], b[2], b[3]);
+            w[e * 2 + 1] = pack4(b[4], b[5], b[6], b[7]);
+          }
+          *reinterpret_cast<uint4*>(kb + (i * 64 + lane) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        m = 0;
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) m = abs_max(abs_max(m, vr[kc][tt][r].x), vr[kc][tt][r].y);
+        sc = block_scale(m, c.act, inv);
+        if (lane == 0) c.vs[at] = sc;
+        uint8_t* vb = c.v + at * (KVB * HD);
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            const int d = kc * 64 + c16 * 4 + z;   // its 8 tokens of this lane group
+            uint32_t w[2];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+              uint32_t b[4];
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const uint32_t x = z < 2 ? vr[kc][tt][r].x : vr[kc][tt][r].y;
+                b[r] = quant(act2f(static_cast<uint16_t>(z & 1 ? x >> 16 : x & 0xFFFFu), c.act), sc, inv);
+              }
+              w[tt] = pack4(b[0], b[1], b[2], b[3]);
+            }
+            *reinterpret_cast<uint2*>(vb + ((d / 32) * 64 + g * 16 + d % 16) * 16 + (d % 32 / 16) * 8) =
+                make_uint2(w[0], w[1]);
+          }
+      }
+    }
+    if (jj != 0 || s.len % KVB == 0) continue;
+    // the tail: the new tokens of the last block, after this wave's own reads of the old one
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    const int t0 = s.len / KVB * KVB > before ? s.len / KVB * KVB : before;
+    for (int x = lane; x < (s.len - t0) * (HD / 8); x += 64) {
+      const int t = t0 + x / (HD / 8), e = x % (HD / 8) * 8;
+      const int64_t r = t - before;
+      *reinterpret_cast<uint4*>(tk + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(kn + r * a.r.k_ld + e);
+      *reinterpret_cast<uint4*>(tv + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(vn + r * a.r.v_ld + e);
+    }
+  }
+}
+
+// (u - 128) * scale in the cache's 16-bit type
+__device__ __forceinline__ uint32_t unq(uint32_t word, int byte, float s, int act) {
+  return f2act((static_cast<float>((word >> (8 * byte)) & 0xFFu) - 128.0f) * s, act);
+}
+
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv_read(KvMoveArgs a) {
+  constexpr int KC = HD / 64;
+  const KvCache& c = a.c;
+  const int n = kv_count(a.b);
+  if (n <= 0) return;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+  const int64_t units = move_count(a.b, n);
+  const int64_t wave = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 6;
+  const int64_t n_waves = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 6;
+  for (int64_t item = wave; item < units * c.n_kv; item += n_waves) {
+    const int64_t u = item / c.n_kv;
+    const int h = static_cast<int>(item - u * c.n_kv);
+    KvSeq s;
+    int jj;
+    if (!move_unit(c, a.b, n, u, s, jj)) continue;
+    const int before = s.len - s.n;
+    const int j = before / KVB + jj;
+    if (j * KVB >= s.len) continue;
+    uint16_t* ko = a.r.k + s.row0 * a.r.k_ld + h * HD;   // row of token `before`
+    uint16_t* vo = a.r.v + s.row0 * a.r.v_ld + h * HD;
+    if ((j + 1) * KVB > s.len) {
+      const uint16_t* tk = tail_at(c, s.tail, 0, h);
+      const uint16_t* tv = tail_at(c, s.tail, 1, h);
+      const int t0 = j * KVB > before ? j * KVB : before;
+      for (int x = lane; x < (s.len - t0) * (HD / 8); x += 64) {
+        const int t = t0 + x / (HD / 8), e = x % (HD / 8) * 8;
+        const int64_t r = t - before;
+        *reinterpret_cast<uint4*>(ko + r * a.r.k_ld + e) = *reinterpret_cast<const uint4*>(tk + t % KVB * HD + e);
+        *reinterpret_cast<uint4*>(vo + r * a.r.v_ld + e) = *reinterpret_cast<const uint4*>(tv + t % KVB * HD + e);
+      }
+      continue;
+    }
+    const int id = kv_block(c, a.b, s.bs + j);
+    if (id < 0) continue;
+    const int64_t at = static_cast<int64_t>(id) * c.n_kv + h;
+    const float ks = c.ks[at], vs = c.vs[at];
+    const uint8_t* kb = c.k + at * (KVB * HD);
+    const uint8_t* vb = c.v + at * (KVB * HD);
+    uint4 kr[2 * KC];
+#pragma unroll
+    for (int i = 0; i < 2 * KC; ++i) kr[i] = *reinterpret_cast<const uint4*>(kb + (i * 64 + lane) * 16);
+    uint2 vr[KC][4];
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        const int d = kc * 64 + c16 * 4 + z;
+        vr[kc][z] = *reinterpret_cast<const uint2*>(vb + ((d / 32) * 64 + g * 16 + d % 16) * 16 + (d % 32 / 16) * 8);
+      }
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const int r = j * KVB + tt * 16 + c16 - before;
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) {
+        const uint32_t x[4] = {kr[tt * KC + kc].x, kr[tt * KC + kc].y, kr[tt * KC + kc].z, kr[tt * KC + kc].w};
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          w[e] = unq(x[e / 2], e % 2 * 2, ks, c.act) | (unq(x[e / 2], e % 2 * 2 + 1, ks, c.act) << 16);
+        if (r < 0) continue;
+        uint4* o = reinterpret_cast<uint4*>(ko + r * a.r.k_ld + kc * 64 + g * 16);
+        o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      }
+    }
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int r = j * KVB + tt * 16 + g * 4 + r4 - before;
+        if (r < 0) continue;
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) {
+          uint32_t w[4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) w[z] = unq(tt ? vr[kc][z].y : vr[kc][z].x, r4, vs, c.act);
+          *reinterpret_cast<uint2*>(vo + r * a.r.v_ld + kc * 64 + c16 * 4) =
+              make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+        }
+      }
+  }
+}
+
+static int kv_grid(int64_t waves, int cap) {
+  int64_t g = (waves + 3) / 4;
+  if (g < 1) g = 1;
+  return static_cast<int>(g > cap ? cap : g);
+}
+
+hipError_t launch_kv_write(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t s) {
+  if (b.n_seq == 0 || b.n_rows == 0) return hipSuccess;
+  const KvMoveArgs a{c, b, r};
+  const dim3 grid(kv_grid(move_units(b) * c.n_kv, 1 << 16));
+  if (c.hd == 64)
+    hipLaunchKernelGGL((k_kv_write<64>), grid, dim3(256), 0, s, a);
+  else if (c.hd == 128)
+    hipLaunchKernelGGL((k_kv_write<128>), grid, dim3(256), 0, s, a);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t s) {
+  if (b.n_seq == 0 || b.n_rows == 0) return hipSuccess;
+  const KvMoveArgs a{c, b, r};
+  const dim3 grid(kv_grid(move_units(b) * c.n_kv, 1 << 16));
+  if (c.hd == 64)
+    hipLaunchKernelGGL((k_kv_read<64>), grid, dim3(256), 0, s, a);
+  else if (c.hd == 128)
+    hipLaunchKernelGGL((k_kv_read<128>), grid, dim3(256), 0, s, a);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ attention
+// A tile is 16 query rows of a (sequence, K/V head): row r is query r / rep of
+// the sequence's and head r % rep of the group, one per lane column.  A
+// workgroup's four waves share a tile's keys in segments of 512 tokens: wave w
+// takes blocks w, w + 4, .. of the segment, each with a softmax state of its
+// own, folded in order at the segment's end and segment after segment.  The
+// order depends on the keys alone, so with one row per sequence a sequence's
+// bits do not depend on the batch, nor on whether its segments run in one
+// workgroup or (SPLIT, few long sequences) in one each with the fold in a
+// second launch.
+// Per block: s' = log2(e) / sqrt(hd) * k_scale * (q . k_u) + log2(v_scale), the weights
+// p' = 2^(s' - m) against a running reference m, numerator += p' v_u, denominator
+// += sum p' / v_scale: a block's scales cost two multiply-adds per score, the
+// bytes themselves (whole numbers, exact in fp16) go into the matrix products.
+// m follows the maximum only when that is more than 8 above it (so weights
+// stay below 2^8 and, with the fixed factor 2^7, in fp16's normal range down to 2^-29 of
+// the largest).  fp16 holds the weights to 2^-12, as the 16-bit attention does.
+constexpr int KV_SEG = 16;       // blocks per segment
+constexpr float KV_SLACK = 8.0f, KV_UP = 7.0f;
+
+__device__ __forceinline__ float swap_max(float v) {   // over the wave's four lane groups
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float swap_add(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// LDS written by a wave, read by the same wave
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// 8 bytes u = q + 128 as the fp16 values q: 0x64uu is 1024 + u
+__device__ __forceinline__ half8 bytes_f16(uint32_t lo, uint32_t hi) {
+  union {
+    uint32_t w[4];
+    half8 h;
+  } x;
+  x.w[0] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
+  x.w[1] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
+  x.w[2] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
+  x.w[3] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
+  const half8 off = {1152, 1152, 1152, 1152, 1152, 1152, 1152, 1152};
+  return x.h - off;
+}
+
+// softmax state of one row: reference, sum, one value of the numerator
+__device__ __forceinline__ void kv_fold(float& m, float& l, float& o, float mp, float lp, float op) {
+  const float mn = fmaxf(m, mp);
+  const float ref = mn == -INFINITY ? 0.f : mn;
+  const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(mp - ref);
+  l = fmaf(lp, y, l * x);
+  o = fmaf(op, y, o * x);
+  m = mn;
+}
+
+struct KvTile {
+  KvSeq s;
+  int r0, rows;      // first row of the tile (of the sequence's n * rep), rows in it
+  int nb;            // blocks that its last query sees
+  int pos0;          // position of the tile's first query
+};
+
+// Tile u of the batch, or false
+__device__ __forceinline__ bool kv_tile(const KvAttendArgs& a, int n, int rep, int64_t u, int h, KvTile& t) {
+  int i;
+  int64_t k;
+  if (a.b.cu) {
+    i = unit_seq(a.b, n, u, rep, 16, 1);
+    k = u - unit_first(a.b, i, rep, 16, 1);
+  } else {
+    const int tiles = (rep + 15) / 16;
+    i = static_cast<int>(u / tiles);
+    k = u - static_cast<int64_t>(i) * tiles;
+  }
+  if (!kv_seq(a.c, a.b, i, t.s)) {
+    if (!a.b.cu && t.s.len == 0) {   // an empty slot's row
+      t.r0 = static_cast<int>(k) * 16;
+      t.rows = rep - t.r0 < 16 ? rep - t.r0 : 16;
+      t.nb = 0;
+      t.pos0 = 0;
+      t.s.n = 1;
+      return true;
+    }
+    return false;
+  }
+  const int64_t all = static_cast<int64_t>(t.s.n) * rep;
+  if (k * 16 >= all) return false;
+  t.r0 = static_cast<int>(k * 16);
+  t.rows = static_cast<int>(all - t.r0 < 16 ? all - t.r0 : 16);
+  t.pos0 = t.s.len - t.s.n + t.r0 / rep;
+  t.nb = (t.s.len - t.s.n + (t.r0 + t.rows - 1) / rep) / KVB + 1;
+  return true;
+}
+
+template <int HD, bool BF, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a, int64_t n_tiles, int32_t n_seg, int32_t slot_rows) {
+  constexpr int KC = HD / 64, NO = HD / 16;
+  __shared__ __attribute__((aligned(16))) uint16_t vt[KVB * HD];   // the tail's values, for transposing reads
+  __shared__ int bad[KVB];                                         // its tokens with an infinity or NaN
+  extern __shared__ float lds[];
+  float* so = lds;                               // [4][rows][HD]
+  float* sm = lds + 4 * slot_rows * HD;          // [4][rows]
+  float* sl = sm + 4 * slot_rows;
+  float* state = sl + 4 * slot_rows;             // [rows][HD], [2][2][rows]: where a workgroup walks several segments
+  const KvCache& c = a.c;
+  const int n = kv_count(a.b);
+  if (n <= 0) return;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rep = a.n_heads / c.n_kv;
+  const int64_t tiles = a.b.cu ? unit_first(a.b, n, rep, 16, 1) : static_cast<int64_t>(n) * ((rep + 15) / 16);
+  const int64_t items = (tiles < n_tiles ? tiles : n_tiles) * c.n_kv * (SPLIT ? n_seg : 1);
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t unit = SPLIT ? item / n_seg : item;   // (tile, K/V head)
+    const int seg0 = SPLIT ? static_cast<int>(item - unit * n_seg) : 0;
+    const int64_t u = unit / c.n_kv;
+    const int h = static_cast<int>(unit - u * c.n_kv);
+    KvTile t;
+    if (!kv_tile(a, n, rep, u, h, t)) continue;
+    const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
+    if (SPLIT && seg0 >= segs) continue;
+    // queries: lane (g, c16) holds row c16, dims 64 kc + 16 g + 8 e .. + 7
+    const int row = t.r0 + (c16 < t.rows ? c16 : 0);
+    const int pos = t.s.len - t.s.n + row / rep;
+    const uint16_t* qp = a.q + (t.s.row0 + row / rep) * a.q_ld + (h * rep + row % rep) * HD + g * 16;
+    float fac = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
+    half8 qf[KC * 2];
+#pragma unroll
+    for (int x = 0; x < KC * 2; ++x) {
+      const uint4 v = *reinterpret_cast<const uint4*>(qp + (x / 2) * 64 + (x % 2) * 8);
+      qf[x] = __builtin_bit_cast(half8, v);
+    }
+    if (BF) {   // the row times a power of two, exact in fp16 (but for values 2^-25 of the row's largest)
+      float mx = 0.f;
+#pragma unroll
+      for (int x = 0; x < KC * 2; ++x) {
+        const uint4 v = __builtin_bit_cast(uint4, qf[x]);
+        const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          mx = fmaxf(mx, fabsf(__uint_as_float(y[e] << 16)));
+          mx = fmaxf(mx, fabsf(__uint_as_float(y[e] & 0xFFFF0000u)));
+        }
+      }
+      mx = swap_max(mx);
+      int ex = static_cast<int>(__float_as_uint(mx) >> 23) - 127;   // mx in [2^ex, 2^(ex + 1))
+      ex = ex < -100 ? -100 : ex;
+      const float up = __uint_as_float(static_cast<uint32_t>(127 + 8 - ex) << 23);
+      fac *= __uint_as_float(static_cast<uint32_t>(127 - 8 + ex) << 23);
+#pragma unroll
+      for (int x = 0; x < KC * 2; ++x) {
+        const uint4 v = __builtin_bit_cast(uint4, qf[x]);
+        const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          qf[x][2 * e] = static_cast<_Float16>(__uint_as_float(y[e] << 16) * up);
+          qf[x][2 * e + 1] = static_cast<_Float16>(__uint_as_float(y[e] & 0xFFFF0000u) * up);
+        }
+      }
+    }
+    const int seg_end = SPLIT ? seg0 + 1 : segs;
+    for (int seg = seg0; seg < (segs == 0 ? seg0 + 1 : seg_end); ++seg) {
+      // the segment's blocks: number, scales
+      const int jl = seg * KV_SEG + lane;
+      int id = -1;
+      float ksl = 0.f, vsl = 1.f;
+      if (lane < KV_SEG && jl < t.nb && (jl + 1) * KVB <= t.s.len) {
+        id = kv_block(c, a.b, t.s.bs + jl);
+        if (id >= 0) {
+          const int64_t at = static_cast<int64_t>(id) * c.n_kv + h;
+          ksl = c.ks[at];
+          vsl = c.vs[at];
+        }
+      }
+      f32x4 o[NO];
+#pragma unroll
+      for (int x = 0; x < NO; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+      float m = -INFINITY, l = 0.f;
+      // weights of the block's 8 tokens of this lane, from its scores acc (times c1, plus c2)
+      auto weigh = [&](const f32x4 (&acc)[2], float c1, float c2, float inv, int tok0, bool masked, float (&p)[8]) {
+        float s[8], mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s[e] = fmaf(acc[e / 4][e % 4], c1, c2);
+          if (masked && tok0 + (e / 4) * 16 + g * 4 + e % 4 > pos) s[e] = -INFINITY;
+          mx = fmaxf(mx, s[e]);
+        }
+        if (__any(mx > m + KV_SLACK)) {
+          const float mn = fmaxf(m, swap_max(mx));
+          const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+#pragma unroll
+          for (int x = 0; x < NO; ++x) o[x] *= al;
+          l *= al;
+          m = mn;
+        }
+        const float ref = m == -INFINITY ? 0.f : m - KV_UP;
+        float ps = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(s[e] - ref);
+          ps += p[e];
+        }
+        l = ps == 0.f ? l : fmaf(ps, inv, l);   // (a block that the row does not see adds nothing, whatever its scale)
+      };
+      for (int k = w; k < KV_SEG; k += 4) {
+        const int j = seg * KV_SEG + k;
+        if (j >= t.nb) break;
+        const int tok0 = j * KVB;
+        f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        float p[8];
+        if (tok0 + KVB <= t.s.len) {
+          const int bid = __builtin_amdgcn_readlane(id, k);
+          if (bid < 0) continue;
+          const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ksl), k));
+          const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vsl), k));
+          const int64_t at = (static_cast<int64_t>(bid) * c.n_kv + h) * (KVB * HD);
+          uint4 kr[2 * KC], vr[2 * KC];
+#pragma unroll
+          for (int x = 0; x < 2 * KC; ++x) kr[x] = *reinterpret_cast<const uint4*>(c.k + at + (x * 64 + lane) * 16);
+#pragma unroll
+          for (int x = 0; x < 2 * KC; ++x) vr[x] = *reinterpret_cast<const uint4*>(c.v + at + (x * 64 + lane) * 16);
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int kc = 0; kc < KC; ++kc) {
+              const uint4 y = kr[tt * KC + kc];
+              acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.x, y.y), qf[kc * 2], acc[tt], 0, 0, 0);
+              acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.z, y.w), qf[kc * 2 + 1], acc[tt], 0, 0, 0);
+            }
+          weigh(acc, fac * ks, __builtin_amdgcn_logf(vs), 1.0f / vs, tok0, tok0 + KVB - 1 > t.pos0, p);
+          half8 pf;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pf[e] = static_cast<_Float16>(p[e]);
+#pragma unroll
+          for (int x = 0; x < 2 * KC; ++x) {
+            o[2 * x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].x, vr[x].y), pf, o[2 * x], 0, 0, 0);
+            o[2 * x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].z, vr[x].w), pf, o[2 * x + 1], 0, 0, 0);
+          }
+        } else {
+          // the tail: 16-bit rows, products in their own type; rows past the length are not read.
+          // Values go through LDS, row-major, in 16-byte pieces (swizzled by the row).
+          const int left = t.s.len - tok0;
+          const uint16_t* tk = tail_at(c, t.s.tail, 0, h);
+          const uint16_t* tv = tail_at(c, t.s.tail, 1, h);
+          const bool several = a.b.cu != nullptr;
+          if (several) bad[lane & (KVB - 1)] = 0;
+          wave_sync();
+#pragma unroll
+          for (int x = lane; x < KVB * HD / 8; x += 64) {
+            const int tok = x / (HD / 8), ch = x % (HD / 8);
+            uint4 y = make_uint4(0, 0, 0, 0);
+            if (tok < left) y = *reinterpret_cast<const uint4*>(tv + tok * HD + ch * 8);
+            if (several) {   // a later query's infinity or NaN must not meet the weight 0
+              const uint32_t m = abs_max(abs_max(abs_max(abs_max(0, y.x), y.y), y.z), y.w), inf = BF ? 0x7F80u : 0x7C00u;
+              if ((m & 0xFFFFu) >= inf || (m >> 16) >= inf) {
+                y = make_uint4(0, 0, 0, 0);
+                bad[tok] = 1;
+              }
+            }
+            *reinterpret_cast<uint4*>(vt + tok * HD + ((ch ^ (tok & 7)) << 3)) = y;
+          }
+          wave_sync();
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt) {
+            const int tok = tt * 16 + c16;
+#pragma unroll
+            for (int x = 0; x < 2 * KC; ++x) {
+              const int e = (x / 2) * 64 + g * 16 + (x % 2) * 8;
+              uint4 y = make_uint4(0, 0, 0, 0);
+              if (tok < left) y = *reinterpret_cast<const uint4*>(tk + tok * HD + e);
+              if (BF) {
+                const uint4 qv = *reinterpret_cast<const uint4*>(qp + (x / 2) * 64 + (x % 2) * 8);
+                acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y),
+                                                                  __builtin_bit_cast(bf16x8, qv), acc[tt], 0, 0, 0);
+              } else {
+                acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, y), qf[x], acc[tt], 0, 0, 0);
+              }
+            }
+          }
+          weigh(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, tok0, true, p);
+          union {
+            uint16_t u[8];
+            half8 h;
+            bf16x8 b;
+          } pf;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            pf.u[e] = BF ? f2bf(p[e]) : f2h(p[e]);
+            if (several && p[e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l = __uint_as_float(0x7FC00000u);
+          }
+          // lane 4 a + b of a 16-lane group receives element b of the pieces that lanes a, a + 4, .. address
+          lds_u16* const vl = (lds_u16*)(vt);
+#pragma unroll
+          for (int x = 0; x < NO; ++x) {
+            v4i16 part[2];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+              const int tok = tt * 16 + g * 4 + (c16 >> 2), d = x * 16 + 4 * (c16 & 3);
+              part[tt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  reinterpret_cast<lds_v4i16*>(vl + tok * HD + (((d >> 3) ^ (tok & 7)) << 3) + (d & 7)));
+            }
+            const auto vf = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            o[x] = BF ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf.b, o[x], 0, 0, 0)
+                      : __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vf), pf.h, o[x], 0, 0, 0);
+          }
+        }
+      }
+      l = swap_add(l);
+      __syncthreads();   // the last segment's states are read before these are written
+      if (c16 < t.rows) {
+#pragma unroll
+        for (int x = 0; x < NO; ++x)
+          *reinterpret_cast<f32x4*>(so + (w * slot_rows + c16) * HD + x * 16 + g * 4) = o[x];
+        if (g == 0) {
+          sm[w * slot_rows + c16] = m;
+          sl[w * slot_rows + c16] = l;
+        }
+      }
+      __syncthreads();
+      // the shares folded in order, then onto the earlier segments' state (kept in LDS, its sums by parity)
+      for (int e = threadIdx.x; e < t.rows * HD; e += 256) {
+        const int r = e / HD, d = e % HD;
+        float m1 = -INFINITY, l1 = 0.f, o1 = 0.f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          kv_fold(m1, l1, o1, sm[v * slot_rows + r], sl[v * slot_rows + r], so[(v * slot_rows + r) * HD + d]);
+        float m0 = -INFINITY, l0 = 0.f, o0 = 0.f;
+        if (!SPLIT && seg > 0) {
+          const float* st = state + slot_rows * HD + (seg & 1) * 2 * slot_rows;
+          m0 = st[r];
+          l0 = st[slot_rows + r];
+          o0 = state[e];
+        }
+        kv_fold(m0, l0, o0, m1, l1, o1);
+        if (!SPLIT && seg + 1 < seg_end) {
+          float* st = state + slot_rows * HD + ((seg + 1) & 1) * 2 * slot_rows;
+          state[e] = o0;
+          if (d == 0) {
+            st[r] = m0;
+            st[slot_rows + r] = l0;
+          }
+        } else if (SPLIT) {   // the segment's state: values, then (reference, sum) per row
+          float* slot = a.part + (unit * n_seg + seg0) * (static_cast<int64_t>(slot_rows) * (HD + 2));
+          slot[e] = o0;
+          if (d == 0) {
+            slot[slot_rows * HD + 2 * r] = m0;
+            slot[slot_rows * HD + 2 * r + 1] = l0;
+          }
+        } else {
+          const int q = t.r0 + r;
+          const float v = l0 == 0.f ? 0.f : o0 / l0;
+          a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Folds the segments' states of each tile, in order.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles, int32_t n_seg, int32_t slot_rows) {
+  const KvCache& c = a.c;
+  const int n = kv_count(a.b);
+  if (n <= 0) return;
+  const int rep = a.n_heads / c.n_kv;
+  const int64_t unit = blockIdx.x;
+  const int64_t u = unit / c.n_kv;
+  const int h = static_cast<int>(unit - u * c.n_kv);
+  const int64_t tiles = a.b.cu ? unit_first(a.b, n, rep, 16, 1) : static_cast<int64_t>(n) * ((rep + 15) / 16);
+  if (u >= tiles || u >= n_tiles) return;
+  KvTile t;
+  if (!kv_tile(a, n, rep, u, h, t)) return;
+  const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
+  const int64_t step = static_cast<int64_t>(slot_rows) * (HD + 2);
+  for (int e = threadIdx.x; e < t.rows * HD; e += 256) {
+    const int r = e / HD, d = e % HD, q = t.r0 + r;
+    const float* slot = a.part + unit * n_seg * step;
+    float m = -INFINITY, l = 0.f, o = 0.f;
+    for (int s = 0; s < segs; ++s, slot += step)
+      kv_fold(m, l, o, slot[slot_rows * HD + 2 * r], slot[slot_rows * HD + 2 * r + 1], slot[e]);
+    const float v = l == 0.f ? 0.f : o / l;
+    a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
+  }
+}
+
+struct KvShape {
+  int64_t tiles;     // bound on the batch's tiles
+  int32_t n_seg;     // segments of the longest sequence
+  int32_t rows;      // rows of a tile that can be in use
+  bool split;
+};
+static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
+  const int rep = n_heads / c.n_kv;
+  KvShape s;
+  s.tiles = b.cu ? b.n_rows * rep / 16 + b.n_seq : static_cast<int64_t>(b.n_seq) * ((rep + 15) / 16);
+  s.n_seg = (b.max_len + KV_SEG * KVB - 1) / (KV_SEG * KVB);
+  s.rows = b.cu || rep > 16 ? 16 : rep;
+  // segments in workgroups of their own where the tiles alone leave CUs without work
+  s.split = s.n_seg > 1 && s.tiles * c.n_kv < 1024 && !b.n_ptr;
+  return s;
+}
+
+size_t kv_attend_part_bytes(const KvCache& c, const KvBatch& b, int32_t n_heads) {
+  const KvShape s = kv_shape(c, b, n_heads);
+  if (!s.split) return 0;
+  return static_cast<size_t>(s.tiles) * c.n_kv * s.n_seg * s.rows * (c.hd + 2) * 4;
+}
+
+hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t s) {
+  if (a.b.n_seq == 0 || a.b.n_rows == 0) return hipSuccess;
+  const KvShape k = kv_shape(a.c, a.b, a.n_heads);
+  if (k.split && !a.part) return hipErrorInvalidValue;
+  const int64_t items = k.tiles * a.c.n_kv * (k.split ? k.n_seg : 1);
+  const dim3 grid(static_cast<unsigned>(items < (1 << 20) ? items : 1 << 20));
+  const bool walks = !k.split && k.n_seg > 1;
+  const size_t lds = static_cast<size_t>(k.rows) * (4 * (a.c.hd + 2) + (walks ? a.c.hd + 4 : 0)) * 4;
+  const bool bf = a.c.act == ACT_BF16;
+#define AIQ_KV_ATTEND(HD_, BF_, SP_) \
+  hipLaunchKernelGGL((k_kv_attend<HD_, BF_, SP_>), grid, dim3(256), lds, s, a, k.tiles, k.n_seg, k.rows)
+#define AIQ_KV_ATTEND_HD(HD_)                             \
+  if (bf && k.split) AIQ_KV_ATTEND(HD_, true, true);      \
+  else if (bf) AIQ_KV_ATTEND(HD_, true, false);           \
+  else if (k.split) AIQ_KV_ATTEND(HD_, false, true);      \
+  else AIQ_KV_ATTEND(HD_, false, false)
+  if (a.c.hd == 64) {
+    AIQ_KV_ATTEND_HD(64);
+  } else if (a.c.hd == 128) {
+    AIQ_KV_ATTEND_HD(128);
+  } else {
+    return hipErrorInvalidValue;
+  }
+#undef AIQ_KV_ATTEND_HD
+#undef AIQ_KV_ATTEND
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !k.split) return e;
+  const dim3 jg(static_cast<unsigned>(k.tiles * a.c.n_kv));
+  if (a.c.hd == 64)
+    hipLaunchKernelGGL((k_kv_join<64>), jg, dim3(256), 0, s, a, k.tiles, k.n_seg, k.rows);
+  else
+    hipLaunchKernelGGL((k_kv_join<128>), jg, dim3(256), 0, s, a, k.tiles, k.n_seg, k.rows);
+  return hipGetLastError();
+}
+
+}  // namespace aiq

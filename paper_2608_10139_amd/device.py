@@ -13,6 +13,7 @@ Inputs are plain host structures:
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 
 import numpy as np
@@ -26,6 +27,7 @@ _DECISION = {"binary_gt": B.AIQ_DECIDE_BINARY_GT, "argmax": B.AIQ_DECIDE_ARGMAX}
 _AGG = {"count": B.AIQ_AGG_COUNT, "avg_label_count_by": B.AIQ_AGG_AVG_LABEL_COUNT_BY,
         "count_by_payload": B.AIQ_AGG_COUNT_BY_PAYLOAD, "sum_f32": B.AIQ_AGG_SUM_F32}
 _LIST_KEYS = ("offsets", "tokens")
+_TORCH_DTYPE = {torch.float32: B.AIQ_F32, torch.float16: B.AIQ_F16, torch.bfloat16: B.AIQ_BF16}
 
 
 def _dev(a: np.ndarray, device) -> torch.Tensor:
@@ -343,3 +345,162 @@ class DevicePrefill:
             self.close()
         except Exception:
             pass
+
+
+def _need(t: torch.Tensor, device, dtype, what: str) -> torch.Tensor:
+    if t.device != device or t.dtype != dtype:
+        raise ValueError(f"{what}: {dtype} on {device} wanted, got {t.dtype} on {t.device}")
+    return t
+
+
+class KvBatch:
+    """The sequences of a call on a DeviceKvCache (see DeviceKvCache.batch)."""
+
+    def __init__(self, struct: B.aiq_kv_batch, keep: tuple):
+        self.struct = struct
+        self.keep = keep      # the tensors that the struct points into
+        self.n_rows = int(struct.n_rows)
+
+
+class DeviceKvCache:
+    """Keys and values of many sequences in 8 bits, in blocks of 32 tokens with
+    one scale per block and K/V head; the tokens of a last block that is not
+    full yet are kept in 16 bits, one tail per sequence (include/aiq.h,
+    aiq_kv_cache).  Rows are tensors [rows, heads, head_dim] of the cache's
+    dtype whose heads lie next to each other (any row stride that is a multiple
+    of 8: they may be columns of q|k|v rows)."""
+
+    def __init__(self, n_blocks: int, n_tails: int, n_kv_heads: int, head_dim: int, dtype=torch.float16, device="cuda"):
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError(f"keys and values are float16 or bfloat16, not {dtype}")
+        self.device = _device(device)
+        self.n_kv_heads, self.head_dim, self.dtype = int(n_kv_heads), int(head_dim), dtype
+        nb, nt = int(n_blocks), int(n_tails)
+        size = (nb, self.n_kv_heads, B.AIQ_KV_BLOCK * self.head_dim)
+        # zeros, so that blocks that were never written read back as zeros
+        self.k = torch.zeros(size, dtype=torch.uint8, device=self.device)
+        self.v = torch.zeros(size, dtype=torch.uint8, device=self.device)
+        self.k_scale = torch.zeros(size[:2], dtype=torch.float32, device=self.device)
+        self.v_scale = torch.zeros(size[:2], dtype=torch.float32, device=self.device)
+        self.tail = torch.zeros((nt, 2, self.n_kv_heads, B.AIQ_KV_BLOCK, self.head_dim), dtype=dtype, device=self.device)
+        self.status = torch.zeros(1, dtype=torch.int64, device=self.device)   # AIQ_DEV_KV_RANGE
+        c = B.aiq_kv_cache()
+        c.k, c.v, c.k_scale, c.v_scale, c.tail = (_ptr(t) for t in (self.k, self.v, self.k_scale, self.v_scale, self.tail))
+        c.n_blocks, c.n_tails, c.n_kv_heads, c.head_dim, c.dtype = nb, nt, self.n_kv_heads, self.head_dim, _TORCH_DTYPE[dtype]
+        self.struct = c
+
+    def batch(self, length: torch.Tensor, blk_start: torch.Tensor, max_len: int, cu: torch.Tensor | None = None,
+              n_rows: int | None = None, blk_ids: torch.Tensor | None = None,
+              tail_ids: torch.Tensor | None = None) -> KvBatch:
+        """Sequence i holds length[i] tokens once the call's rows cu[i] ..
+        cu[i+1] are in (cu None: row i is its last token; length 0 is an empty
+        slot), in the blocks blk_ids[blk_start[i] .. blk_start[i+1]] (None: the
+        numbers themselves), with tail tail_ids[i] (None: i).  All int32
+        tensors on the cache's device; they may change between calls, within
+        max_len tokens and n_rows rows (None with cu: cu's last value is read
+        back once, here).  The tensors are kept, not copied."""
+        n = int(length.numel())
+        for t, want, what in ((length, n, "length"), (blk_start, n + 1, "blk_start"), (cu, n + 1, "cu"),
+                              (blk_ids, None, "blk_ids"), (tail_ids, n, "tail_ids")):
+            if t is None:
+                continue
+            _need(t, self.device, torch.int32, what)
+            if not t.is_contiguous() or (want is not None and t.numel() != want):
+                raise ValueError(f"{what}: {want} contiguous values wanted, got {tuple(t.shape)}")
+        b = B.aiq_kv_batch()
+        b.n_seq, b.max_len = n, int(max_len)
+        b.n_rows = n if cu is None else int(cu[-1].item()) if n_rows is None else int(n_rows)
+        b.len, b.cu, b.blk_start, b.blk_ids, b.tail_ids = (_ptr(t) for t in (length, cu, blk_start, blk_ids, tail_ids))
+        b.status = _ptr(self.status)
+        return KvBatch(b, (length, blk_start, cu, blk_ids, tail_ids))
+
+    def _rows(self, t: torch.Tensor, n_rows: int, heads: int | None, what: str) -> int:
+        """Elements between rows of t [n_rows, heads, head_dim]."""
+        _need(t, self.device, self.dtype, what)
+        if t.dim() != 3 or t.shape[0] != n_rows or t.shape[2] != self.head_dim or (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{what}: [{n_rows}, {heads or 'heads'}, {self.head_dim}] wanted, got {tuple(t.shape)}")
+        if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim)):
+            raise ValueError(f"{what}: a row's heads must lie next to each other (strides {t.stride()})")
+        width = t.shape[1] * self.head_dim
+        return t.stride(0) if t.shape[0] > 1 else width
+
+    def write(self, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+        """Appends the batch's rows."""
+        ks, vs = (self._rows(t, batch.n_rows, self.n_kv_heads, w) for t, w in ((k, "k"), (v, "v")))
+        with _on(self.device, stream) as s:
+            B.aiq_kv_write(self.struct, batch.struct, _ptr(k), ks, _ptr(v), vs, s)
+
+    def read(self, batch: KvBatch, stream=None) -> tuple:
+        """The batch's rows as the cache holds them: (k, v)."""
+        w = self.n_kv_heads * self.head_dim
+        with _on(self.device, stream) as s:
+            k, v = (torch.empty((batch.n_rows, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device)
+                    for _ in range(2))
+            B.aiq_kv_read(self.struct, batch.struct, _ptr(k), w, _ptr(v), w, s)
+        return k, v
+
+    def attend(self, batch: KvBatch, q: torch.Tensor, out: torch.Tensor | None = None,
+               out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
+        """Attention of the batch's rows q [rows, heads, head_dim] over the
+        cache (their own tokens included), in out_dtype (default the cache's)."""
+        qs = self._rows(q, batch.n_rows, None, "q")
+        heads = q.shape[1]
+        if out is not None and (out.shape != q.shape or not out.is_contiguous() or out.device != self.device):
+            raise ValueError(f"out: contiguous {tuple(q.shape)} on {self.device} wanted")
+        dtype = out.dtype if out is not None else out_dtype or self.dtype
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError(f"out is float16 or bfloat16, not {dtype}")
+        need = B.aiq_kv_attend_workspace_size(self.struct, batch.struct, heads)
+        with _on(self.device, stream) as s:   # the workspace belongs to the stream that uses it
+            if out is None:
+                out = torch.empty(q.shape, dtype=dtype, device=self.device)
+            ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+            B.aiq_kv_attend(self.struct, batch.struct, _ptr(q), qs, heads, _ptr(out), heads * self.head_dim,
+                            _TORCH_DTYPE[dtype], _ptr(ws), need, s)
+        return out
+
+
+@contextlib.contextmanager
+def _on(device: torch.device, stream):
+    """The device's given or current stream, current while tensors are
+    allocated (they belong to the stream that uses them) and work is enqueued."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream(device).cuda_stream
+        else:
+            with torch.cuda.stream(stream):
+                yield stream.cuda_stream
+
+
+def _device(device) -> torch.device:
+    d = torch.device(device)
+    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor | None, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+           min_p: float = 0.0, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The next token of each row of logits [rows, vocab] (float32, float16 or
+    bfloat16; any row stride) with the random numbers u [rows] (float32 in
+    [0, 1)): int32 [rows] (include/aiq.h, aiq_sample)."""
+    if logits.dim() != 2 or logits.dtype not in _TORCH_DTYPE or logits.stride(1) != 1 and logits.numel():
+        raise ValueError(f"logits: rows of float32, float16 or bfloat16 wanted, got {tuple(logits.shape)} {logits.dtype}")
+    n, vocab = logits.shape
+    dev = logits.device
+    if dev.type != "cuda":
+        raise ValueError("logits must be on a GPU")
+    if u is not None:
+        _need(u, dev, torch.float32, "u")
+        if u.shape != (n,) or not u.is_contiguous():
+            raise ValueError(f"u: {n} contiguous values wanted")
+    if out is not None:
+        _need(out, dev, torch.int32, "out")
+        if out.shape != (n,) or not out.is_contiguous():
+            raise ValueError(f"out: {n} contiguous values wanted")
+    p = B.aiq_sampling()
+    p.temperature, p.top_p, p.min_p, p.top_k = float(temperature), float(top_p), float(min_p), int(top_k)
+    with _on(dev, stream) as s:
+        if out is None:
+            out = torch.empty(n, dtype=torch.int32, device=dev)
+        B.aiq_sample(_ptr(logits), _TORCH_DTYPE[logits.dtype], logits.stride(0) if n > 1 else vocab, vocab, n, p, _ptr(u),
+                     _ptr(out), s)
+    return out

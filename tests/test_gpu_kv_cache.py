@@ -1,0 +1,374 @@
+"""The 8-bit key/value cache: written and read back, and attention over it,
+against a plain form in 64 bits.
+
+Read-back is exact: the whole numbers and scales are defined step by step.
+Attention: weights reach the products in 16 bits (half a step each, u_p: fp16
+2^-11; a bf16 cache's tail 2^-8) while their sum stays in 32, so the output
+moves by at most u_p max|v|; scores of up to 2^6 in 32 bits move a weight by
+less than 2^-15, 2^-14 with the sum's; the output's own rounding is u_out |out|."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_10139_amd import binding as B
+from paper_2608_10139_amd.device import DeviceKvCache
+from tests import _kv_ref as R
+
+pytestmark = pytest.mark.gpu
+BLOCK = R.BLOCK
+U = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def i32(x):
+    return torch.as_tensor(np.ascontiguousarray(x), dtype=torch.int32).cuda()
+
+
+def starts(n):
+    out = np.zeros(len(n) + 1, np.int64)
+    out[1:] = np.cumsum(n)
+    return out
+
+
+class Case:
+    """Sequences of the given final lengths in one cache: their rows (host and
+    device), blocks in a shuffled order, tails too."""
+
+    def __init__(self, lens, heads, kv, hd, dtype, seed, paged=True, spare=0):
+        r = np.random.default_rng(seed)
+        self.lens, self.heads, self.kv, self.hd, self.dtype = np.asarray(lens), heads, kv, hd, dtype
+        n = len(lens)
+        size = np.exp(0.5 * r.standard_normal((1, kv, hd)))
+        self.k = [torch.tensor(r.standard_normal((L, kv, hd)) * size, dtype=dtype) for L in lens]
+        self.v = [torch.tensor(r.standard_normal((L, kv, hd)) * r.uniform(0.1, 4.0, (1, kv, 1)), dtype=dtype) for L in lens]
+        self.q = [torch.tensor(r.standard_normal((L, heads, hd)) * 1.5, dtype=dtype) for L in lens]
+        blocks = (self.lens + BLOCK - 1) // BLOCK + spare
+        self.start = starts(blocks)
+        nb = int(self.start[-1])
+        self.blk_start = i32(self.start)
+        self.blk_ids = i32(r.permutation(nb)) if paged else None
+        self.tail_ids = i32(r.permutation(n)) if paged else None
+        self.cache = DeviceKvCache(max(nb, 1), max(n, 1), kv, hd, dtype)
+
+    def batch(self, length, new, single=False):
+        length, new = np.asarray(length), np.asarray(new)
+        return self.cache.batch(i32(length), self.blk_start, int(max(self.lens.max(initial=0), 1)),
+                                cu=None if single else i32(starts(new)), blk_ids=self.blk_ids, tail_ids=self.tail_ids)
+
+    def rows(self, what, length, new):
+        """The last new[i] of the first length[i] rows of every sequence, in a wider matrix's columns."""
+        x = getattr(self, what)
+        parts = [x[i][L - m:L] for i, (L, m) in enumerate(zip(length, new))]
+        flat = torch.cat(parts) if parts else x[0][:0]
+        n, h = flat.shape[0], flat.shape[1]
+        wide = torch.full((n, (h + 2) * self.hd), 7.0, dtype=self.dtype)
+        wide[:, self.hd:(h + 1) * self.hd] = flat.reshape(n, -1)
+        return wide.cuda()[:, self.hd:(h + 1) * self.hd].unflatten(1, (h, self.hd))
+
+    def write(self, length, new, single=False):
+        self.cache.write(self.batch(length, new, single), self.rows("k", length, new), self.rows("v", length, new))
+
+    def ok(self):
+        assert int(self.cache.status.item()) == 0
+
+    def held(self, i, L=None):
+        """What the cache should hold of sequence i once L tokens are in: (k, v) float64."""
+        L = self.lens[i] if L is None else L
+        return tuple(R.held(x[i][:L].float().numpy()) for x in (self.k, self.v))
+
+    def check_read(self, length):
+        k, v = self.cache.read(self.batch(length, length))
+        at = starts(length)
+        for i, L in enumerate(length):
+            for got, want in zip((k, v), self.held(i, L)):
+                want = torch.from_numpy(want).to(torch.float32).to(self.dtype)   # exact in 32 bits, rounded once
+                assert torch.equal(got[at[i]:at[i + 1]].cpu(), want), f"sequence {i} of {L} tokens"
+        self.ok()
+
+    def check_attend(self, length, new, out, out_dtype=None):
+        u_p, u_o = U[self.dtype], U[out_dtype or self.dtype]
+        at = starts(new)
+        out = out.double().cpu().numpy()
+        for i, (L, m) in enumerate(zip(length, new)):
+            if m == 0:
+                continue
+            want, top = R.attend(self.q[i][L - m:L].float().numpy(), *self.held(i, L), np.arange(L - m, L))
+            tol = (u_p + 2.0 ** -14) * top[:, :, None] + u_o * np.abs(want) + 1e-7
+            err = np.abs(out[at[i]:at[i + 1]] - want)
+            assert np.all(err <= tol), f"sequence {i} of {L} tokens: {np.nanmax(err / tol):.2f} of the bound"
+        self.ok()
+
+
+LENS = [1, 31, 32, 33, 0, 64, 65, 100, 257, 2]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("kv,hd", [(8, 64), (3, 128), (1, 64)])
+def test_written_rows_read_back(kv, hd, dtype):
+    say("case: write and read", kv, hd, dtype)
+    c = Case(LENS, kv, kv, hd, dtype, 1)
+    c.write(c.lens, c.lens)
+    c.check_read(c.lens)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_what_is_held_does_not_depend_on_the_calls(hd):
+    """Rows in pieces of many sizes, then one by one: the same bytes as at once."""
+    say("case: pieces", hd)
+    lens = np.array([97, 160, 64, 33, 70])
+    one, many = (Case(lens, 2, 2, hd, torch.float16, 2, spare=s) for s in (0, 0))
+    one.write(lens, lens)
+    held = np.zeros(len(lens), np.int64)
+    r = np.random.default_rng(3)
+    while np.any(held < lens - 3):
+        new = np.minimum(r.integers(0, 70, len(lens)), np.maximum(lens - 3 - held, 0))
+        held = held + new
+        many.write(held, new)
+    for _ in range(3):
+        held = held + 1
+        many.write(held, np.ones_like(held), single=True)
+    for a, b in ((one.cache.k, many.cache.k), (one.cache.v, many.cache.v), (one.cache.k_scale, many.cache.k_scale),
+                 (one.cache.v_scale, many.cache.v_scale)):
+        assert torch.equal(a, b)
+    many.check_read(lens)
+
+
+def test_scales_of_extreme_blocks():
+    """Zeros, the largest numbers, subnormals, one large value among small ones, infinity and NaN."""
+    say("case: extreme blocks")
+    for dtype, big in ((torch.float16, 65504.0), (torch.bfloat16, 3.0e38)):
+        c = Case([7 * 32], 1, 1, 64, dtype, 4, paged=False)
+        k = c.k[0]
+        k[:32] = 0.0
+        k[32:64] = (k[32:64].double() / k[32:64].double().abs().max() * big).to(dtype)
+        k[64:96] *= 2.0 ** -22 if dtype == torch.float16 else 2.0 ** -130
+        k[96:128] *= 1e-3
+        k[100, 0, 5] = 500.0
+        k[128 + 3, 0, 9] = float("inf")
+        k[160 + 31, 0, 63] = float("nan")
+        c.write(c.lens, c.lens)
+        got = c.cache.read(c.batch(c.lens, c.lens))[0].cpu()
+        want = torch.from_numpy(c.held(0)[0]).to(torch.float32).to(dtype)
+        assert torch.equal(got[:128], want[:128]) and torch.equal(got[192:], want[192:])
+        assert torch.isnan(got[128:192]).all()
+        x = k[:128].double()
+        step = x.reshape(4, -1).abs().max(1).values.repeat_interleave(32)[:, None, None] / 127
+        lost = 2.0 ** -81 if dtype == torch.bfloat16 else 0.0
+        assert torch.all((got[:128].double() - x).abs() <= 0.5001 * step + U[dtype] * x.abs() + U[dtype] * step + lost + 2.0 ** -25)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("heads,kv,hd", [(8, 8, 64), (32, 8, 64), (6, 2, 128), (20, 1, 64), (16, 1, 128)])
+def test_attention_of_single_tokens(heads, kv, hd, dtype):
+    say("case: single tokens", heads, kv, hd, dtype)
+    c = Case([1, 2, 31, 32, 33, 64, 95, 511, 512, 513, 1100], heads, kv, hd, dtype, 5)
+    c.write(c.lens, c.lens)
+    one = np.ones_like(c.lens)
+    out = c.cache.attend(c.batch(c.lens, one, single=True), c.rows("q", c.lens, one))
+    c.check_attend(c.lens, one, out)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("heads,kv,hd", [(8, 8, 64), (24, 8, 128), (8, 1, 64)])
+def test_attention_of_several_tokens(heads, kv, hd, dtype):
+    say("case: several tokens", heads, kv, hd, dtype)
+    c = Case([1, 5, 33, 64, 130, 0, 200, 620], heads, kv, hd, dtype, 6)
+    new = np.array([1, 5, 2, 64, 17, 0, 33, 40])
+    c.write(c.lens, c.lens)
+    out = c.cache.attend(c.batch(c.lens, new), c.rows("q", c.lens, new))
+    c.check_attend(c.lens, new, out)
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float16, torch.bfloat16])
+def test_attention_output_type(out_dtype):
+    say("case: output type", out_dtype)
+    c = Case([40, 7], 4, 2, 64, torch.float16, 7)
+    c.write(c.lens, c.lens)
+    new = np.array([1, 1])
+    out = c.cache.attend(c.batch(c.lens, new), c.rows("q", c.lens, new), out_dtype=out_dtype)
+    assert out.dtype == out_dtype
+    c.check_attend(c.lens, new, out, out_dtype)
+
+
+def test_empty_slots_and_rows_behind_the_last():
+    say("case: empty slots")
+    c = Case([40, 0, 64, 0], 4, 2, 64, torch.float16, 8)
+    one = np.ones(4, np.int64)
+    c.write(c.lens, c.lens)
+    before = [t.clone() for t in (c.cache.k, c.cache.tail)]
+    q = torch.randn(4, 4, 64, device="cuda").half()
+    q[0], q[2] = c.q[0][39], c.q[2][63]
+    out = torch.full((6, 4, 64), 5.0, dtype=torch.float16, device="cuda")
+    c.cache.attend(c.batch(c.lens, one, single=True), q, out=out[:4])
+    assert torch.all(out[1] == 0) and torch.all(out[3] == 0) and torch.all(out[4:] == 5.0)
+    c.check_attend(c.lens, [1, 0, 1, 0], out[[0, 2]])
+    # an empty slot writes nothing; no sequence, no row: nothing at all
+    c.cache.write(c.batch([0, 0, 0, 0], one, single=True), q[:, :2], q[:, :2])
+    c.cache.write(c.batch([0, 0, 0, 0], [0, 0, 0, 0]), q[:0, :2], q[:0, :2])
+    for a, b in zip(before, (c.cache.k, c.cache.tail)):
+        assert torch.equal(a, b)
+    none = DeviceKvCache(0, 0, 2, 64)
+    b = none.batch(i32([]), i32([0]), 0)
+    assert none.attend(b, q[:0]).shape == (0, 4, 64) and none.read(b)[0].shape == (0, 2, 64)
+    c.ok()
+
+
+def test_long_sequence_alone_and_among_others_gives_the_same_bits():
+    """Split between workgroups where it is alone, walked by one among 1,100 others."""
+    say("case: long sequence alone and in a batch")
+    n = 1100
+    lens = np.full(n, 3)
+    lens[7] = 3000
+    c = Case(lens, 3, 1, 64, torch.float16, 9)
+    c.write(lens, lens)
+    one = np.ones(n, np.int64)
+    b = c.batch(lens, one, single=True)
+    assert B.aiq_kv_attend_workspace_size(c.cache.struct, b.struct, 3) == 0
+    many = c.cache.attend(b, c.rows("q", lens, one))
+    s, e = c.start[7], c.start[8]
+    alone = c.cache.batch(i32([3000]), i32([0, e - s]), 3000, blk_ids=c.blk_ids[s:e].contiguous(),
+                          tail_ids=c.tail_ids[7:8].contiguous())
+    assert B.aiq_kv_attend_workspace_size(c.cache.struct, alone.struct, 3) > 0
+    out = c.cache.attend(alone, c.q[7][-1:].cuda())
+    assert torch.equal(out[0], many[7])
+    want, top = R.attend(c.q[7][-1:].float().numpy(), *c.held(7), [2999])
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= (2.0 ** -11 + 2.0 ** -14) * top[:, :, None] + 2.0 ** -11 * np.abs(want))
+    c.ok()
+
+
+def test_infinity_and_nan_behind_a_query_stay_there():
+    """Later tokens of the batch hold NaN and infinities: in a later block, and in the tail."""
+    say("case: NaN behind")
+    for where in (70, 100):   # in a full block; in the tail
+        c = Case([110], 4, 2, 64, torch.float16, 10, paged=False)
+        c.k[0][where:, :, 3], c.v[0][where:, :, 5] = float("nan"), float("inf")
+        c.write([110], [110])
+        out = c.cache.attend(c.batch([110], [110]), c.rows("q", [110], [110]))
+        first = where // 32 * 32 if where < 96 else where   # a block's poison is the whole block's
+        c.check_attend([first], [first], out[:first])
+        assert torch.isnan(out[where + 1:]).all()
+
+
+def test_scores_far_apart():
+    """One key takes all the weight, late or early; keys of very different blocks."""
+    say("case: scores far apart")
+    for at in (0, 40, 599):
+        c = Case([600], 2, 1, 64, torch.float16, 11, paged=False)
+        c.q[0] *= 0.5
+        c.k[0][at] = c.q[0][599][:1] * 40
+        c.v[0][32:64] *= 2.0 ** -9
+        c.write([600], [600])
+        out = c.cache.attend(c.batch([600], [1]), c.rows("q", [600], [1]))
+        c.check_attend([600], [1], out)
+
+
+def test_shared_blocks():
+    """Two sequences with the first 64 tokens in the same blocks."""
+    say("case: shared prefix blocks")
+    c = Case([64, 90, 75], 4, 2, 64, torch.bfloat16, 12, paged=False)
+    for x in (c.k, c.v):
+        x[1][:64], x[2][:64] = x[0], x[0]
+    c.write([64, 0, 0], [64, 0, 0])
+    # sequences 1 and 2: the two shared blocks, then one of their own
+    b = lambda new: c.cache.batch(i32([90, 75]), i32([0, 3, 6]), 90, cu=i32(starts(new)), blk_ids=i32([0, 1, 2, 0, 1, 5]),   # noqa: E731
+                                  tail_ids=i32([2, 0]))
+    c.cache.write(b([26, 11]), *(torch.cat((x[1][64:], x[2][64:75])).cuda() for x in (c.k, c.v)))
+    out = c.cache.attend(b([1, 2]), torch.cat((c.q[1][89:], c.q[2][73:75])).cuda())
+    c.check_attend([0, 90, 75], [0, 1, 2], out)
+
+
+def test_cache_beyond_32_bit_offsets():
+    """Blocks above 2 GiB of bytes (and 2^31 elements) from the start."""
+    say("case: 70,000 blocks of 8 heads of 128")
+    cache = DeviceKvCache(70000, 1, 8, 128)
+    c = Case([100], 8, 8, 128, torch.float16, 13, paged=False)
+    b = lambda new: cache.batch(i32([100]), i32([0, 4]), 100, cu=i32([0, new]), blk_ids=i32([69999, 3, 69998, 69000]))   # noqa: E731
+    cache.write(b(100), c.k[0].cuda(), c.v[0].cuda())
+    k, v = cache.read(b(100))
+    for got, want in zip((k, v), c.held(0)):
+        assert torch.equal(got.cpu(), torch.from_numpy(want).float().half())
+    c.check_attend([100], [1], cache.attend(b(1), c.q[0][99:].cuda()))
+
+
+def test_numbers_out_of_bounds_are_flagged_and_left_out():
+    """Every one is kept from the memory by the kernels' own checks."""
+    say("case: bad batches")
+    c = Case([70, 40], 2, 2, 64, torch.float16, 14, paged=False)
+    c.write(c.lens, c.lens)
+    want = c.cache.attend(c.batch(c.lens, [1, 1]), c.rows("q", c.lens, [1, 1]))
+    q = c.rows("q", c.lens, [1, 1])
+    bad = [dict(length=[200, 40]), dict(length=[-1, 40]), dict(length=[0, 40], cu=[0, 1, 2]), dict(blk_ids=[0, 99, 2, 3, 4]),
+           dict(blk_ids=[0, -5, 2, 3, 4]), dict(tail_ids=[7, 1]), dict(tail_ids=[-1, 1]), dict(blk_start=[0, 1, 5]),
+           dict(blk_start=[-3, 3, 5], start0=True)]
+    for d in bad:
+        say("  ", d)
+        kv = (c.cache.k.clone(), c.cache.v.clone(), c.cache.tail.clone())
+        b = c.cache.batch(i32(d.get("length", [70, 40])), i32(d.get("blk_start", [0, 3, 5])), 128,
+                          cu=i32(d.get("cu", [0, 1, 2])), blk_ids=i32(d["blk_ids"]) if "blk_ids" in d else None,
+                          tail_ids=i32(d["tail_ids"]) if "tail_ids" in d else None)
+        if "blk_start" in d and not d.get("start0"):
+            want_1 = None    # sequence 1's blocks moved too
+        else:
+            want_1 = want[1]
+        out = c.cache.attend(b, q)
+        c.cache.read(b)
+        assert int(c.cache.status.item()) == B.AIQ_DEV_KV_RANGE
+        if want_1 is not None:
+            assert torch.equal(out[1], want_1)   # the other sequence is not harmed
+        c.cache.write(b, c.rows("k", c.lens, [1, 1]), c.rows("v", c.lens, [1, 1]))   # (its last row again)
+        for x, y in zip(kv, (c.cache.k, c.cache.v, c.cache.tail)):
+            assert torch.equal(x, y)
+        c.cache.status.zero_()
+
+
+def test_captured_steps_replay_as_eager_ones():
+    """A step (write, attend) captured once and replayed as the sequences grow,
+    with eager work between, on a stream of its own."""
+    say("case: captured steps")
+    lens = np.array([62, 600, 95, 31])
+    c, e = (Case(lens + 40, 6, 2, 128, torch.bfloat16, 15) for _ in range(2))
+    for x in (c, e):
+        x.write(lens, lens)
+    one = np.ones(4, np.int64)
+    length = i32(lens)
+    b = c.cache.batch(length, c.blk_start, 700, blk_ids=c.blk_ids, tail_ids=c.tail_ids)
+    k, v, q = (torch.zeros(4, h, 128, dtype=torch.bfloat16, device="cuda") for h in (2, 2, 6))
+    out = torch.zeros_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.cache.attend(b, q, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        length.add_(1)
+        c.cache.write(b, k, v)
+        c.cache.attend(b, q, out=out)
+    for step in range(1, 40):
+        at = lens + step
+        for t, what in ((k, "k"), (v, "v"), (q, "q")):
+            t.copy_(c.rows(what, at, one))
+        g.replay()
+        e.write(at, one, single=True)
+        want = e.cache.attend(e.batch(at, one, single=True), e.rows("q", at, one))
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), step
+    c.check_read(lens + 39)
+
+
+def test_a_stream_of_its_own():
+    say("case: side stream")
+    c = Case([50, 700], 4, 2, 64, torch.float16, 16)
+    one = np.ones(2, np.int64)
+    k, v, q = (c.rows(w, c.lens, c.lens) for w in "kvq")
+    ball, bone = c.batch(c.lens, c.lens), c.batch(c.lens, one, single=True)
+    q1 = c.rows("q", c.lens, one)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    c.cache.write(ball, k, v, stream=s)
+    out = c.cache.attend(bone, q1, stream=s)
+    s.synchronize()
+    c.check_attend(c.lens, one, out)
