@@ -182,6 +182,15 @@ typedef struct aiq_model {
   const void* lm_head;           /* device [vocab, d] */
 } aiq_model;
 
+/* Decoding by sampling instead of by the maximum (see aiq_sample). */
+typedef struct aiq_sampling {
+  double temperature;
+  double top_p;              /* 1 = off */
+  double min_p;              /* 0 = off */
+  int32_t top_k;             /* 0 = off */
+  int32_t reserved;
+} aiq_sampling;
+
 typedef struct aiq_query {
   int32_t n_pred;
   aiq_pred preds[AIQ_MAX_PREDS];       /* conjunction over probe columns */
@@ -220,7 +229,7 @@ typedef struct aiq_query {
   /* AI_TRANSFORM (Table 1; Section 4, Q3 and Q5).  gen_tokens > 0 replaces
      the label decision: every selected row's sequence is continued by up
      to gen_tokens tokens, each the argmax of the last position's logits over
-     the whole vocabulary (ties to the lowest id); a row's generation stops
+     the whole vocabulary (ties to the lowest id), or drawn (sample, below); a row's generation stops
      after eos_id (kept as its last token) and its later slots hold pad_id.
      A row is kept iff its generated tokens (up to the end) contain
      like[0..n_like) contiguously (LIKE '%pattern%' on token ids); with
@@ -246,6 +255,16 @@ typedef struct aiq_query {
   int32_t pairs;
   int32_t pair_key_col;
   int64_t max_pairs;
+  /* AI_TRANSFORM by sampling: sample = 1 draws each generated token from the
+     last position's logits as aiq_sample does, instead of taking their
+     argmax.  Token g of probe row r uses the random number sample_u[r *
+     gen_tokens + g], a device array [n_rows, gen_tokens] in [0, 1), so a row's
+     tokens do not depend on which other rows are selected.  sample_u may be
+     NULL at temperature 0 (the argmax).  AIQ_EINVAL without generation or for values that
+     aiq_sample refuses. */
+  int32_t sample;
+  aiq_sampling sampling;
+  const float* sample_u;
 } aiq_query;
 
 typedef struct aiq_plan_opts {
@@ -253,8 +272,21 @@ typedef struct aiq_plan_opts {
   int32_t n_layers_override;           /* diagnostics: 0 = every layer, n > 0 = the first n
                                           layers, negative = no layer (embedding -> head) */
   int32_t flags;                       /* AIQ_PLAN_* bits */
-  int32_t reserved[4];
+  int32_t kv_dtype;                    /* AI_TRANSFORM: keys and values that generation steps read, 0 or
+                                          AIQ_F16: in 16 bits; AIQ_I8: in 8 bits (see below) */
+  int32_t reserved[3];
 } aiq_plan_opts;
+
+/*
+ * aiq_plan_opts.kv_dtype = AIQ_I8: every layer's keys and values of the prompt
+ * (a shared prefix included) and of generated tokens go into a cache of the form of
+ * aiq_kv_cache, written and attended over by the kernels behind aiq_kv_write
+ * and aiq_kv_attend, instead of staying in the 16-bit q|k|v rows: half the
+ * bytes per step and, as queries are not kept, less than half the workspace
+ * per prompt token.  Prefill attention still uses the 16-bit rows, so the first
+ * generated token is the same; later ones see 8-bit keys and values.  Requires
+ * gen_tokens > 0 (AIQ_EINVAL otherwise).
+ */
 
 /*
  * AIQ_PLAN_RELATIONAL_ONLY: aiq_run executes only the relational part of the
@@ -373,7 +405,7 @@ enum {
   AIQ_K_HEAD = 9,
   AIQ_K_AGG = 10,
   AIQ_K_DECODE = 11,      /* AI_TRANSFORM generation steps: embedding, projections, norms */
-  AIQ_K_DECODE_ATTN = 12, /* ... their attention over the kept keys and values */
+  AIQ_K_DECODE_ATTN = 12, /* ... their attention over the kept keys and values; writes to an 8-bit cache */
   AIQ_K_DECODE_HEAD = 13, /* ... the full-vocabulary head and argmax; the LIKE match */
   AIQ_K_LAST = 14         /* the last layer after its q|k|v projection, last positions only */
 };
@@ -641,14 +673,6 @@ aiq_status aiq_kv_attend(const aiq_kv_cache* cache, const aiq_kv_batch* batch, c
  * outside (0, 1], min_p outside [0, 1], logits not aligned to their type),
  * AIQ_EUNSUPPORTED (dtype), AIQ_EHIP.
  */
-typedef struct aiq_sampling {
-  double temperature;
-  double top_p;              /* 1 = off */
-  double min_p;              /* 0 = off */
-  int32_t top_k;             /* 0 = off */
-  int32_t reserved;
-} aiq_sampling;
-
 aiq_status aiq_sample(const void* logits, int32_t dtype, int64_t ld, int32_t vocab, int64_t n_rows,
                       const aiq_sampling* sampling, const float* u, int32_t* token, void* stream);
 

@@ -70,6 +70,11 @@ class aiq_model(C.Structure):
                 ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
 
 
+class aiq_sampling(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 class aiq_query(C.Structure):
     _fields_ = [("n_pred", C.c_int32), ("preds", aiq_pred * AIQ_MAX_PREDS),
                 ("join", C.c_int32), ("probe_key_col", C.c_int32), ("build_key_col", C.c_int32),
@@ -80,12 +85,13 @@ class aiq_query(C.Structure):
                 ("decision", C.c_int32), ("agg", C.c_int32), ("group_col", C.c_int32),
                 ("n_group_keys", C.c_int32), ("gen_tokens", C.c_int32), ("eos_id", C.c_int32),
                 ("pad_id", C.c_int32), ("n_like", C.c_int32), ("like", C.c_int32 * AIQ_MAX_LIKE),
-                ("pairs", C.c_int32), ("pair_key_col", C.c_int32), ("max_pairs", C.c_int64)]
+                ("pairs", C.c_int32), ("pair_key_col", C.c_int32), ("max_pairs", C.c_int64),
+                ("sample", C.c_int32), ("sampling", aiq_sampling), ("sample_u", C.c_void_p)]
 
 
 class aiq_plan_opts(C.Structure):
     _fields_ = [("chunk_tokens", C.c_int64), ("n_layers_override", C.c_int32), ("flags", C.c_int32),
-                ("reserved", C.c_int32 * 4)]
+                ("kv_dtype", C.c_int32), ("reserved", C.c_int32 * 3)]
 
 
 class aiq_out(C.Structure):
@@ -112,11 +118,6 @@ class aiq_kv_batch(C.Structure):
     _fields_ = [("n_seq", C.c_int32), ("max_len", C.c_int32), ("n_rows", C.c_int64), ("len", C.c_void_p),
                 ("cu", C.c_void_p), ("blk_start", C.c_void_p), ("blk_ids", C.c_void_p), ("tail_ids", C.c_void_p),
                 ("status", C.c_void_p)]
-
-
-class aiq_sampling(C.Structure):
-    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32),
-                ("reserved", C.c_int32)]
 
 
 EXPORTS = ("aiq_plan_create", "aiq_workspace_size", "aiq_plan_passes", "aiq_plan_chunk_tokens",

@@ -38,6 +38,7 @@ struct aiq_plan {
   bool pairs = false;     // Q4: the sequences are candidate pairs of selected rows
   int64_t n_seq_ub = 0;   // upper bound on sequences: selected rows, or max_pairs
   int32_t gen_blocks = 0; // row blocks of the full-vocabulary head
+  bool kv8 = false;       // AI_TRANSFORM: keys and values of generation steps in 8 bits
   aiq_table probe{}, build{};
   std::vector<aiq_col> probe_cols, build_cols;
   aiq_query q{};
@@ -61,6 +62,11 @@ struct aiq_plan {
 namespace {
 
 constexpr size_t ALIGN = 256;
+
+bool sampling_ok(const aiq_sampling& s) {
+  return s.temperature >= 0.0 && std::isfinite(s.temperature) && s.top_p > 0.0 && s.top_p <= 1.0 && s.min_p >= 0.0 &&
+         s.min_p <= 1.0 && s.top_k >= 0;
+}
 
 struct Carver {
   size_t off = 0;
@@ -161,6 +167,7 @@ struct Layout {
   size_t ctr, mask, blk_cnt, blk_off, sel, payload, lens, label, logits, cu, blk_tok, tok_off, packed, hkeys, hvals,
       bins, desc, rcos, rsin, rrev, x, delta, h, qkv, att, ffn, pos, hf, ssp, rs, pkv, ptok, pcu, pdesc, pxlast,
       kvc, gkv, glog, gdone, gen, gdesc, gcnt, kcount, koff, prank, psorted, pcnt, poff, pscan, pa, pb,
+      k8, v8, ks8, vs8, tail8, plen, pcu32, pblk, stok,
       lb, xl, ldesc, laux, jkeys, jvals, jlog2, gslot, gkey0, gval0, gkey1, gval1, ghist, gn, total;
 };
 
@@ -223,6 +230,11 @@ void take_last(const aiq_plan* p, Carver& c, Layout& L, int64_t seq) {
   L.ldesc = c.take(static_cast<size_t>(last_blocks(seq)) * D_STRIDE * 8);
   // row scales and positions of the last positions of every block (GEMM tiles read 256 rows)
   if (p->q_last_only) L.laux = c.take(static_cast<size_t>(std::max<int64_t>(seq, 1) + 256) * 8);
+}
+
+// blocks of one layer's 8-bit cache for any chunk
+int64_t kv8_blocks(const aiq_plan* p) {
+  return kv_plan_blocks(p->t_cap, p->seq_ub, p->share_prefix ? p->prefix.n : 0, p->gen);
 }
 
 Layout run_layout(const aiq_plan* p) {
@@ -298,10 +310,28 @@ Layout run_layout(const aiq_plan* p) {
   }
   if (p->gen > 0) {   // AI_TRANSFORM: kept prompt keys / values, generated-token cache, head, tokens
     const size_t G = static_cast<size_t>(p->gen), su = static_cast<size_t>(p->seq_ub);
-    L.kvc = c.take(static_cast<size_t>(p->n_layers) * p->t_cap * p->n_qkv * ab);
-    L.gkv = c.take(static_cast<size_t>(p->n_layers) * su * G * 2 * p->d_kv * ab);
+    if (p->kv8) {   // every layer's blocks, scales and tails; the chunk's lengths and block numbers
+      const size_t layers = static_cast<size_t>(p->n_layers), nb = static_cast<size_t>(kv8_blocks(p));
+      const size_t heads = static_cast<size_t>(p->model.n_kv_heads);
+      L.k8 = c.take(layers * nb * AIQ_KV_BLOCK * p->d_kv);
+      L.v8 = c.take(layers * nb * AIQ_KV_BLOCK * p->d_kv);
+      L.ks8 = c.take(layers * nb * heads * 4);
+      L.vs8 = c.take(layers * nb * heads * 4);
+      L.tail8 = c.take(layers * su * 2 * AIQ_KV_BLOCK * p->d_kv * 2);
+      L.plen = c.take(su * 4);
+      L.pcu32 = c.take((su + 1) * 4);
+      L.pblk = c.take((su + 1) * 4);
+    } else {
+      L.kvc = c.take(static_cast<size_t>(p->n_layers) * p->t_cap * p->n_qkv * ab);
+      L.gkv = c.take(static_cast<size_t>(p->n_layers) * su * G * 2 * p->d_kv * ab);
+    }
     L.hf = c.take(su * d * ab);
-    L.glog = c.take(std::min<size_t>(su, GEN_HEAD_ROWS) * (p->model.vocab / 64) * 8);   // per-64-column maxima
+    if (p->q.sample) {   // fp32 logits of a head block, drawn tokens
+      L.glog = c.take(std::min<size_t>(su, GEN_HEAD_ROWS) * p->model.vocab * 4);
+      L.stok = c.take(std::min<size_t>(su, GEN_HEAD_ROWS) * 4);
+    } else {
+      L.glog = c.take(std::min<size_t>(su, GEN_HEAD_ROWS) * (p->model.vocab / 64) * 8);   // per-64-column maxima
+    }
     L.gdone = c.take(su * 4);
     L.gen = c.take(static_cast<size_t>(n + 1) * G * 4);
     L.gdesc = c.take(D_STRIDE * 8);
@@ -357,6 +387,37 @@ struct Tracer {
   }
 };
 
+// Layer l of a generation plan's 8-bit cache.
+KvCache kv8_layer(const aiq_plan* p, void* ws, const Layout& L, int l) {
+  const size_t nb = static_cast<size_t>(kv8_blocks(p)), heads = static_cast<size_t>(p->model.n_kv_heads);
+  KvCache c{};
+  c.k = at<uint8_t>(ws, L.k8) + l * nb * AIQ_KV_BLOCK * p->d_kv;
+  c.v = at<uint8_t>(ws, L.v8) + l * nb * AIQ_KV_BLOCK * p->d_kv;
+  c.ks = at<float>(ws, L.ks8) + l * nb * heads;
+  c.vs = at<float>(ws, L.vs8) + l * nb * heads;
+  c.tail = at<uint16_t>(ws, L.tail8) + static_cast<size_t>(l) * p->seq_ub * 2 * AIQ_KV_BLOCK * p->d_kv;
+  c.n_blocks = static_cast<int32_t>(nb);
+  c.n_tails = static_cast<int32_t>(p->seq_ub);
+  c.n_kv = p->model.n_kv_heads;
+  c.hd = p->hd;
+  c.act = 2;   // q|k|v rows are fp16 whatever the projections' type
+  return c;
+}
+
+// The chunk's sequences: n_seq of them (device), prompts first (cu set: rows
+// of the chunk behind npre common ones), single tokens later.
+KvBatch kv8_batch(const aiq_plan* p, void* ws, const Layout& L, const int64_t* n_seq, int64_t* ctr) {
+  KvBatch b{};
+  b.n_seq = static_cast<int32_t>(p->seq_ub);
+  b.max_len = p->max_seq + p->gen;
+  b.n_rows = p->seq_ub;
+  b.n_ptr = n_seq;
+  b.len = at<int32_t>(ws, L.plen);
+  b.blk_start = at<int32_t>(ws, L.pblk);
+  b.status = ctr + C_STATUS;
+  return b;
+}
+
 #define HIP_TRY(expr)                         \
   do {                                        \
     if ((expr) != hipSuccess) return AIQ_EHIP; \
@@ -382,6 +443,7 @@ struct PrefixUse {
   int32_t npre = 0;
   const float* x_pre = nullptr;
   bool head = true;
+  bool kv8 = false;   // the row passes write keys and values into the 8-bit cache
 };
 
 // Enqueues embedding, the layer stack and the label head for one chunk.
@@ -531,6 +593,21 @@ aiq_status enqueue_chunk(const aiq_plan* p, void* ws, const Layout& L, int64_t* 
       } else {
         TRACED(tr, AIQ_K_GEMM_QKV, gemm(EPI_QKV_ROPE, h, d, p->n_qkv, d, W.wq, W.wk, W.wv, qkv_l, p->n_qkv, nullptr,
                                         nullptr, 0, nullptr, false, fold && l > 0));
+      }
+      if (pu.kv8) {
+        KvBatch kb = kv8_batch(p, ws, L, desc + D_NSEQ, ctr);
+        kb.cu = at<int32_t>(ws, L.pcu32);
+        kb.n_rows = t_cap;
+        KvRows kr{};
+        kr.k = static_cast<uint16_t*>(qkv_l) + p->d_q;
+        kr.v = kr.k + p->d_kv;
+        kr.k_ld = kr.v_ld = p->n_qkv;
+        if (pu.pkv_layers) {
+          kb.n_pre = pu.npre;
+          kr.pk = reinterpret_cast<const uint16_t*>(static_cast<const char*>(pu.pkv_layers) + l * pre_layer) + p->d_q;
+          kr.pv = kr.pk + p->d_kv;
+        }
+        TRACED(tr, AIQ_K_DECODE_ATTN, launch_kv_write(kv8_layer(p, ws, L, l), kb, kr, s));
       }
       AttnArgs aa{};
       aa.qkv = qkv_l;
@@ -682,7 +759,7 @@ aiq_status enqueue_chunk(const aiq_plan* p, void* ws, const Layout& L, int64_t* 
 // row to hf): the first token from hf, then gen - 1 steps of one row per
 // sequence through the layer stack and the full-vocabulary head.
 aiq_status enqueue_generation(const aiq_plan* p, void* ws, const Layout& L, const int64_t* cdesc, const int64_t* cu,
-                              const PrefixUse& pu, Tracer& tr, hipStream_t s) {
+                              const PrefixUse& pu, int64_t* ctr, Tracer& tr, hipStream_t s) {
   const aiq_model& m = p->model;
   const aiq_query& q = p->q;
   const int d = m.d_model, G = p->gen;
@@ -741,15 +818,38 @@ aiq_status enqueue_generation(const aiq_plan* p, void* ws, const Layout& L, cons
   };
   const bool fold = su <= RS_FOLD_ROWS;   // row scales taken where they are used
   const float* g0 = p->n_layers > 0 ? p->layers[0].attn_norm : m.final_norm;
-  // full-vocabulary head over hf in row blocks, argmax into generated slot
-  // `step`, the embedding of the next step's row
+  // full-vocabulary head over hf in row blocks, argmax (or a draw) into
+  // generated slot `step`, the embedding of the next step's row
   auto next_tokens = [&](int step) -> aiq_status {
     for (int b = 0; b < p->gen_blocks; ++b) {
       const int64_t row0 = static_cast<int64_t>(b) * GEN_HEAD_ROWS;
-      TRACED(tr, AIQ_K_DECODE_HEAD, gemm(EPI_ARGMAX, static_cast<const char*>(hf) + row0 * d * ab, d, cnt + b,
-                                         std::min<int64_t>(su - row0, GEN_HEAD_ROWS), m.vocab, d, m.lm_head,
-                                         nullptr, nullptr, logits, m.vocab / 64, nullptr, false));
+      const int64_t rows_ub = std::min<int64_t>(su - row0, GEN_HEAD_ROWS);
+      TRACED(tr, AIQ_K_DECODE_HEAD, gemm(q.sample ? EPI_STORE_F32 : EPI_ARGMAX,
+                                         static_cast<const char*>(hf) + row0 * d * ab, d, cnt + b, rows_ub, m.vocab, d,
+                                         m.lm_head, nullptr, nullptr, logits, q.sample ? m.vocab : m.vocab / 64,
+                                         nullptr, false));
       GenNextArgs na{};
+      if (q.sample) {
+        SampleArgs sa{};
+        sa.logits = logits;
+        sa.dtype = AIQ_F32;
+        sa.ld = sa.vocab = m.vocab;
+        sa.n_rows = rows_ub;
+        sa.n_ptr = cnt + b;
+        sa.temperature = q.sampling.temperature;
+        sa.top_p = q.sampling.top_p;
+        sa.min_p = q.sampling.min_p;
+        sa.top_k = q.sampling.top_k >= m.vocab ? 0 : q.sampling.top_k;
+        sa.u = q.sample_u;
+        sa.u_row = at<int32_t>(ws, L.sel);
+        sa.u_base = gd + D_SEQ_BEGIN;
+        sa.u_add = row0;
+        sa.u_ld = G;
+        sa.u_at = step;
+        sa.token = at<int32_t>(ws, L.stok);
+        TRACED(tr, AIQ_K_DECODE_HEAD, launch_sample(sa, s));
+        na.tok = sa.token;
+      }
       na.part = logits;
       na.vocab = m.vocab;
       na.cnt = cnt + b;
@@ -789,6 +889,24 @@ aiq_status enqueue_generation(const aiq_plan* p, void* ws, const Layout& L, cons
       const bool last = l + 1 == p->n_layers;
       TRACED(tr, AIQ_K_DECODE, gemm(EPI_QKV_ROPE, h, d, n_rows, su, p->n_qkv, d, W.wq, W.wk, W.wv, qkv, p->n_qkv,
                                     nullptr, false, fold && l > 0));
+      if (p->kv8) {
+        KvAttendArgs ka{};
+        ka.c = kv8_layer(p, ws, L, l);
+        ka.b = kv8_batch(p, ws, L, n_rows, ctr);
+        ka.b.len_add = k + 1;
+        KvRows kr{};
+        kr.k = static_cast<uint16_t*>(qkv) + p->d_q;
+        kr.v = kr.k + p->d_kv;
+        kr.k_ld = kr.v_ld = p->n_qkv;
+        TRACED(tr, AIQ_K_DECODE_ATTN, launch_kv_write(ka.c, ka.b, kr, s));
+        ka.q = static_cast<const uint16_t*>(qkv);
+        ka.q_ld = p->n_qkv;
+        ka.n_heads = m.n_heads;
+        ka.out = static_cast<uint16_t*>(att);
+        ka.out_ld = p->d_q;
+        ka.out_act = p->act;
+        TRACED(tr, AIQ_K_DECODE_ATTN, launch_kv_attend(ka, s));
+      } else {
       GenAttnArgs ga{};
       ga.qkv = qkv;
       ga.kvc = static_cast<const char*>(pu.qkv_layers) + l * kv_layer;
@@ -808,6 +926,7 @@ aiq_status enqueue_generation(const aiq_plan* p, void* ws, const Layout& L, cons
       ga.out_act = p->act;
       ga.seq_ub = su;
       TRACED(tr, AIQ_K_DECODE_ATTN, launch_attention_gen(ga, s));
+      }
       TRACED(tr, AIQ_K_DECODE, gemm(EPI_RESID, att, p->d_q, n_rows, su, d, p->d_q, W.wo, nullptr, nullptr, nullptr,
                                     d, W.ffn_norm, true));
       if (!fold) TRACED(tr, AIQ_K_DECODE, launch_row_scale(gd, ssp, d / 64, d, eps, rs, su, s));
@@ -890,7 +1009,12 @@ aiq_status aiq_plan_create(const aiq_model* model, const aiq_table* probe, const
       if (q.n_like < 0 || q.n_like > AIQ_MAX_LIKE) return fail(AIQ_EINVAL);
       for (int k = 0; k < q.n_like; ++k)
         if (q.like[k] < 0 || q.like[k] >= model->vocab) return fail(AIQ_EINVAL);
+      if (q.sample != 0 && (q.sample != 1 || !sampling_ok(q.sampling) ||
+                            (q.sampling.temperature > 0.0 && !q.sample_u) ||
+                            reinterpret_cast<uintptr_t>(q.sample_u) % 4))
+        return fail(AIQ_EINVAL);
     } else {
+      if (q.sample != 0) return fail(AIQ_EINVAL);
       if (q.n_labels < 2 || q.n_labels > AIQ_MAX_LABELS) return fail(AIQ_EINVAL);
       for (int k = 0; k < q.n_labels; ++k)
         if (q.label_ids[k] < 0 || q.label_ids[k] >= model->vocab) return fail(AIQ_EINVAL);
@@ -899,6 +1023,10 @@ aiq_status aiq_plan_create(const aiq_model* model, const aiq_table* probe, const
     if (q.n_prefix < 0 || q.n_prefix > AIQ_MAX_PREFIX) return fail(AIQ_EINVAL);
     for (int k = 0; k < q.n_prefix; ++k)
       if (q.prefix[k] < 0 || q.prefix[k] >= model->vocab) return fail(AIQ_EINVAL);
+  }
+  if (opts && opts->kv_dtype != 0 && opts->kv_dtype != AIQ_F16) {
+    if (opts->kv_dtype != AIQ_I8 || p->gen == 0) return fail(AIQ_EINVAL);
+    p->kv8 = true;
   }
   if (probe) {
     if (!query) return fail(AIQ_EINVAL);
@@ -986,7 +1114,8 @@ aiq_status aiq_plan_create(const aiq_model* model, const aiq_table* probe, const
     const int64_t per_tok = static_cast<int64_t>(resid_bytes(p)) +
                             static_cast<int64_t>(model->d_model + p->n_qkv + p->d_q + model->d_ff) *
                                 (p->bf16 ? 2 : 4) + 4 +
-                            (p->gen > 0 ? static_cast<int64_t>(p->n_layers) * p->n_qkv * 2 : 0);
+                            (p->kv8 ? static_cast<int64_t>(p->n_layers) * (2 * p->d_kv + 8 * model->n_kv_heads / AIQ_KV_BLOCK)
+                             : p->gen > 0 ? static_cast<int64_t>(p->n_layers) * p->n_qkv * 2 : 0);
     const int64_t def_chunk = std::min<int64_t>((int64_t(96) << 30) / per_tok, int64_t(4) << 20);
     int64_t ct = (opts && opts->chunk_tokens > 0) ? opts->chunk_tokens : def_chunk;
     ct = std::max<int64_t>(ct, max_packed);
@@ -1001,6 +1130,7 @@ aiq_status aiq_plan_create(const aiq_model* model, const aiq_table* probe, const
     p->gen_blocks = p->gen > 0 ? static_cast<int32_t>((p->seq_ub + GEN_HEAD_ROWS - 1) / GEN_HEAD_ROWS) : 0;
     p->prefix.n = q.n_prefix;
     for (int k = 0; k < q.n_prefix; ++k) p->prefix.tok[k] = q.prefix[k];
+    if (p->kv8 && (kv8_blocks(p) > INT32_MAX || p->t_cap > INT32_MAX)) return fail(AIQ_EUNSUPPORTED);
     // GROUP BY over any int32 key: at most one group per selected row (by
     // probe column) or per build row (by the joined payload)
     if ((q.agg == AIQ_AGG_AVG_LABEL_COUNT_BY || q.agg == AIQ_AGG_COUNT_BY_PAYLOAD) && q.n_group_keys == 0) {
@@ -1219,17 +1349,22 @@ aiq_status aiq_run(const aiq_plan* p, void* ws, size_t ws_bytes, const aiq_out* 
     rows_pu.npre = np;
     rows_pu.x_pre = pxl;
   }
-  if (p->gen > 0) {   // the generation steps read every layer's prompt keys and values
+  if (p->kv8) {
+    rows_pu.kv8 = true;
+  } else if (p->gen > 0) {   // the generation steps read every layer's prompt keys and values
     rows_pu.qkv_layers = at<void>(ws, L.kvc);
     rows_pu.qkv_rows = p->t_cap;
   }
   // ---- prefill + label head (or generation), chunk by chunk
   for (int64_t c = 0; c < p->n_chunks; ++c) {
+    if (p->kv8)
+      TRACED(tr, AIQ_K_PACK, launch_kv_plan(desc + c * D_STRIDE, cu, rows_pu.npre, p->gen, static_cast<int32_t>(p->seq_ub),
+                                            at<int32_t>(ws, L.plen), at<int32_t>(ws, L.pcu32), at<int32_t>(ws, L.pblk), s));
     aiq_status e = enqueue_chunk(p, ws, L, desc + c * D_STRIDE, cu, ctr, packed, p->t_cap, p->seq_ub, label, logits,
                                  p->gen > 0 ? at<void>(ws, L.hf) : nullptr, tr, s, rows_pu);
     if (e != AIQ_OK) return e;
     if (p->gen > 0) {
-      e = enqueue_generation(p, ws, L, desc + c * D_STRIDE, cu, rows_pu, tr, s);
+      e = enqueue_generation(p, ws, L, desc + c * D_STRIDE, cu, rows_pu, ctr, tr, s);
       if (e != AIQ_OK) return e;
     }
   }
@@ -1473,9 +1608,7 @@ aiq_status aiq_sample(const void* logits, int32_t dtype, int64_t ld, int32_t voc
                       const aiq_sampling* sm, const float* u, int32_t* token, void* stream) {
   if (!sm || n_rows < 0 || vocab <= 0 || vocab > (1 << 24) || (ld < vocab && ld != 0)) return AIQ_EINVAL;
   if (dtype != AIQ_F32 && dtype != AIQ_F16 && dtype != AIQ_BF16) return AIQ_EUNSUPPORTED;
-  if (!(sm->temperature >= 0.0) || !std::isfinite(sm->temperature) || !(sm->top_p > 0.0) || !(sm->top_p <= 1.0) ||
-      !(sm->min_p >= 0.0) || !(sm->min_p <= 1.0) || sm->top_k < 0)
-    return AIQ_EINVAL;
+  if (!sampling_ok(*sm)) return AIQ_EINVAL;
   if (n_rows == 0) return AIQ_OK;
   if (!logits || !token || (sm->temperature > 0.0 && !u)) return AIQ_EINVAL;
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == AIQ_F32 ? 4 : 2)) return AIQ_EINVAL;

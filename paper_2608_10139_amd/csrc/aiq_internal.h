@@ -456,6 +456,7 @@ hipError_t launch_norm_rows(const int64_t* gen_desc, const float* x, const float
 // (prompt length incl. a shared prefix of npre tokens, + step).
 struct GenNextArgs {
   const void* part;
+  const int32_t* tok;        // the rows' tokens, drawn already (part unused), or null
   int32_t vocab;
   const int64_t* cnt;        // rows of the block
   int64_t row0;
@@ -491,7 +492,8 @@ hipError_t launch_copy_rows_i32(const int32_t* src, const int64_t* n_ptr, int64_
 // ---------------------------------------------------------------- 8-bit key/value cache
 // aiq_kv_cache and aiq_kv_batch as the kernels take them.  Beyond the public
 // batch: the number of sequences from device memory (n_ptr, else n_seq, which
-// bounds it) and len[i] + len_add for the length.
+// bounds it), len[i] + len_add for the length, and n_pre rows (KvRows::pk, pv,
+// the same for every sequence) before the rows cu[i] .. cu[i+1] of each.
 struct KvCache {
   uint8_t* k;
   uint8_t* v;
@@ -507,6 +509,7 @@ struct KvBatch {
   const int32_t* len;
   int32_t len_add;
   const int32_t* cu;
+  int32_t n_pre;
   const int32_t* blk_start;
   const int32_t* blk_ids;
   const int32_t* tail_ids;
@@ -517,7 +520,19 @@ struct KvRows {
   uint16_t* k;
   uint16_t* v;
   int64_t k_ld, v_ld;
+  const uint16_t* pk;        // the n_pre common rows, k_ld and v_ld apart
+  const uint16_t* pv;
 };
+// The cache batch of a chunk of a generation query: for its sequence i of
+// own(i) tokens behind npre common ones, plen[i] = npre + own(i), cu32[i] = the
+// tokens before it in the chunk, and blk[i] its first block, with room for
+// plen[i] + gen tokens; cu32 and blk have one entry more.  At most
+// kv_plan_blocks(tokens, n, npre, gen) blocks in all.
+hipError_t launch_kv_plan(const int64_t* desc, const int64_t* cu, int32_t npre, int32_t gen, int32_t n_ub,
+                          int32_t* plen, int32_t* cu32, int32_t* blk, hipStream_t s);
+inline int64_t kv_plan_blocks(int64_t tokens, int64_t n, int64_t npre, int64_t gen) {
+  return (tokens + n * (npre + gen)) / AIQ_KV_BLOCK + n;
+}
 hipError_t launch_kv_write(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t s);
 hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t s);
 struct KvAttendArgs {
@@ -545,7 +560,10 @@ struct SampleArgs {
   double temperature;        // 0: the maximum
   double top_p, min_p;
   int32_t top_k;             // 0: off
-  const float* u;
+  const float* u;            // row r's number: u[r], or with u_row u[u_row[*u_base + u_add + r] * u_ld + u_at]
+  const int32_t* u_row;
+  const int64_t* u_base;
+  int64_t u_add, u_ld, u_at;
   int32_t* token;
 };
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s);

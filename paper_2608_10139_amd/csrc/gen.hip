@@ -434,8 +434,8 @@ __global__ __launch_bounds__(256) void k_gen_next(GenNextArgs a) {
   for (int64_t r = wave; r < rows; r += n_waves) {
     const int2* pr = static_cast<const int2*>(a.part) + r * n_chunk;
     float best = -INFINITY;
-    int32_t bi = INT32_MAX;
-    for (int c = lane; c < n_chunk; c += 64) {   // ascending columns: strict > keeps each lane's first maximum
+    int32_t bi = a.tok ? a.tok[r] : INT32_MAX;   // drawn: every lane's
+    for (int c = a.tok ? n_chunk : lane; c < n_chunk; c += 64) {   // ascending columns: strict > keeps each lane's first maximum
       const int2 p = pr[c];
       const float v = __int_as_float(p.x);
       if (v > best) {

@@ -45,7 +45,7 @@ __device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, int i
   if (b.cu) {
     const int c0 = b.cu[i], c1 = b.cu[i + 1];
     s.row0 = c0;
-    s.n = c1 - c0;
+    s.n = c1 - c0 + b.n_pre;
     if (c0 < 0 || c1 < c0 || c1 > b.n_rows) {
       kv_flag(b);
       return false;
@@ -85,7 +85,7 @@ __device__ __forceinline__ int kv_count(const KvBatch& b) {
 // first(i) = per * cu[i] / R + extra * i on, enough for `extra` + its rows / R
 // units; which of them it fills the unit finds out itself.
 __device__ __forceinline__ int64_t unit_first(const KvBatch& b, int i, int per, int R, int extra) {
-  const int64_t c = b.cu[i] < 0 ? 0 : b.cu[i];
+  const int64_t c = (b.cu[i] < 0 ? 0 : b.cu[i]) + static_cast<int64_t>(i) * b.n_pre;
   return c * per / R + static_cast<int64_t>(extra) * i;
 }
 __device__ __forceinline__ int unit_seq(const KvBatch& b, int n, int64_t u, int per, int R, int extra) {
@@ -157,7 +157,7 @@ __device__ __forceinline__ uint16_t* tail_at(const KvCache& c, int tail, int kv,
 
 // work units of a batch: blocks that its rows touch (bound on the host, at most that on the device)
 static __host__ __device__ int64_t move_units(const KvBatch& b) {
-  return b.cu ? b.n_rows / KVB + 2 * static_cast<int64_t>(b.n_seq) : b.n_seq;
+  return b.cu ? (b.n_rows + static_cast<int64_t>(b.n_seq) * b.n_pre) / KVB + 2 * static_cast<int64_t>(b.n_seq) : b.n_seq;
 }
 __device__ __forceinline__ int64_t move_count(const KvBatch& b, int n) {
   const int64_t u = b.cu ? unit_first(b, n, 1, KVB, 2) : n, ub = move_units(b);
@@ -194,13 +194,16 @@ __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
     const int before = s.len - s.n;
     const int j = before / KVB + jj;
     if (j * KVB >= s.len) continue;
-    const uint16_t* kn = a.r.k + s.row0 * a.r.k_ld + h * HD;   // row of token `before`
-    const uint16_t* vn = a.r.v + s.row0 * a.r.v_ld + h * HD;
     uint16_t* tk = tail_at(c, s.tail, 0, h);
     uint16_t* tv = tail_at(c, s.tail, 1, h);
-    auto src = [&](const uint16_t* rows, int64_t ld, const uint16_t* tail, int t) {   // token t of block j
-      const int p = j * KVB + t;
-      return p < before ? tail + t * HD : rows + static_cast<int64_t>(p - before) * ld;
+    // rows of token p, not in the cache before this call
+    auto row_k = [&](int p) {
+      const int64_t r = p - before;
+      return (r < a.b.n_pre ? a.r.pk + r * a.r.k_ld : a.r.k + (s.row0 + r - a.b.n_pre) * a.r.k_ld) + h * HD;
+    };
+    auto row_v = [&](int p) {
+      const int64_t r = p - before;
+      return (r < a.b.n_pre ? a.r.pv + r * a.r.v_ld : a.r.v + (s.row0 + r - a.b.n_pre) * a.r.v_ld) + h * HD;
     };
     if ((j + 1) * KVB <= s.len) {
       const int id = kv_block(c, a.b, s.bs + j);
@@ -210,7 +213,8 @@ __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
         uint32_t m = 0;
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-          const uint16_t* p = src(kn, a.r.k_ld, tk, tt * 16 + c16) + g * 16;
+          const int t = tt * 16 + c16, at_p = j * KVB + t;
+          const uint16_t* p = (at_p < before ? tk + t * HD : row_k(at_p)) + g * 16;
 #pragma unroll
           for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
@@ -221,7 +225,8 @@ __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const uint16_t* p = src(vn, a.r.v_ld, tv, tt * 16 + g * 4 + r) + c16 * 4;
+            const int t = tt * 16 + g * 4 + r, at_p = j * KVB + t;
+            const uint16_t* p = (at_p < before ? tv + t * HD : row_v(at_p)) + c16 * 4;
 #pragma unroll
             for (int kc = 0; kc < KC; ++kc) vr[kc][tt][r] = *reinterpret_cast<const uint2*>(p + kc * 64);
           }
@@ -286,9 +291,8 @@ __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
     const int t0 = s.len / KVB * KVB > before ? s.len / KVB * KVB : before;
     for (int x = lane; x < (s.len - t0) * (HD / 8); x += 64) {
       const int t = t0 + x / (HD / 8), e = x % (HD / 8) * 8;
-      const int64_t r = t - before;
-      *reinterpret_cast<uint4*>(tk + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(kn + r * a.r.k_ld + e);
-      *reinterpret_cast<uint4*>(tv + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(vn + r * a.r.v_ld + e);
+      *reinterpret_cast<uint4*>(tk + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(row_k(t) + e);
+      *reinterpret_cast<uint4*>(tv + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(row_v(t) + e);
     }
   }
 }
@@ -389,15 +393,39 @@ static int kv_grid(int64_t waves, int cap) {
 }
 
 hipError_t launch_kv_write(const KvCache& c, const KvBatch& b, const KvRows& r, hipStream_t s) {
-  if (b.n_seq == 0 || b.n_rows == 0) return hipSuccess;
+  if (b.n_seq == 0 || (b.n_rows == 0 && b.n_pre == 0)) return hipSuccess;
+  if (b.n_pre < 0 || (b.n_pre > 0 && (!b.cu || !r.pk || !r.pv))) return hipErrorInvalidValue;
   const KvMoveArgs a{c, b, r};
-  const dim3 grid(kv_grid(move_units(b) * c.n_kv, 1 << 16));
+  // (a bound from the host only: the sequences may be few)
+  const dim3 grid(kv_grid(move_units(b) * c.n_kv, b.n_ptr ? 1 << 13 : 1 << 16));
   if (c.hd == 64)
     hipLaunchKernelGGL((k_kv_write<64>), grid, dim3(256), 0, s, a);
   else if (c.hd == 128)
     hipLaunchKernelGGL((k_kv_write<128>), grid, dim3(256), 0, s, a);
   else
     return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+__global__ __launch_bounds__(256) void k_kv_plan(const int64_t* desc, const int64_t* cu, int32_t npre, int32_t gen,
+                                                 int32_t n_ub, int32_t* plen, int32_t* cu32, int32_t* blk) {
+  const int64_t sb = desc[D_SEQ_BEGIN], tb = desc[D_TOK_BEGIN], ns = desc[D_NSEQ];
+  const int64_t n = ns < n_ub ? ns : n_ub;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i <= n;
+       i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+    const int64_t c = cu[sb + i] - tb;
+    cu32[i] = static_cast<int32_t>(c);
+    // room for ceil of a sequence's tokens / 32: floors of the running sums differ by its floor at least
+    blk[i] = static_cast<int32_t>((c + i * (npre + gen)) / KVB + i);
+    if (i < n) plen[i] = npre + static_cast<int32_t>(cu[sb + i + 1] - cu[sb + i]);
+  }
+}
+
+hipError_t launch_kv_plan(const int64_t* desc, const int64_t* cu, int32_t npre, int32_t gen, int32_t n_ub,
+                          int32_t* plen, int32_t* cu32, int32_t* blk, hipStream_t s) {
+  const int64_t g = (static_cast<int64_t>(n_ub) + 256) / 256;
+  hipLaunchKernelGGL(k_kv_plan, dim3(static_cast<unsigned>(g < 4096 ? g : 4096)), dim3(256), 0, s, desc, cu, npre, gen,
+                     n_ub, plen, cu32, blk);
   return hipGetLastError();
 }
 

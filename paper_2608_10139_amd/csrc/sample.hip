@@ -262,7 +262,8 @@ __global__ __launch_bounds__(SN) void k_sample(SampleArgs a) {
     uint64_t total = 0;
 #pragma unroll
     for (int x = 0; x < SW; ++x) total += s.wave[x];
-    const double f = static_cast<double>(a.u[r]);
+    const int64_t ui = a.u_row ? a.u_row[*a.u_base + a.u_add + r] * a.u_ld + a.u_at : r;
+    const double f = static_cast<double>(a.u[ui]);
     uint64_t target = total - 1;   // at least 1 kept: the maximum
     if (f < 1.0) {
       const double t = f * static_cast<double>(total);

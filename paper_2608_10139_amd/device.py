@@ -9,7 +9,8 @@ Inputs are plain host structures:
   model  = {"spec": <object with n_layers, d_model, ...>, "emb", "layers": [...],
             "final_norm", "lm_head"} with bf16 weights as uint16 bit patterns
   query  = <object with preds, labels, decision, agg, join, n_prefix, group_col,
-            n_group_keys>
+            n_group_keys; AI_TRANSFORM by sampling: sampling = (temperature, top_k,
+            top_p, min_p)>
 """
 from __future__ import annotations
 
@@ -176,6 +177,11 @@ def make_query(query, probe: DeviceTable | None, build: DeviceTable | None, pref
     q.n_like = len(like)
     for i, t in enumerate(like):
         q.like[i] = int(t)
+    sm = getattr(query, "sampling", None)
+    if sm is not None:
+        q.sample = 1
+        q.sampling.temperature, q.sampling.top_k = float(sm[0]), int(sm[1])
+        q.sampling.top_p, q.sampling.min_p = float(sm[2]), float(sm[3])
     if getattr(query, "pair_key", None):
         q.pairs = 1
         q.pair_key_col = probe.index[query.pair_key]
@@ -184,19 +190,32 @@ def make_query(query, probe: DeviceTable | None, build: DeviceTable | None, pref
 
 
 class DeviceQuery:
-    """A planned query over device-resident tables and weights."""
+    """A planned query over device-resident tables and weights.
+
+    AI_TRANSFORM queries: ``kv_dtype`` "i8" keeps the keys and values that
+    generation steps read in 8 bits (default 16); ``sample_u`` [probe rows,
+    gen_tokens] holds the random numbers of a query that samples."""
 
     def __init__(self, tables: dict, model, query, device="cuda", chunk_tokens: int = 0,
                  n_layers: int | None = None, dmodel: DeviceModel | None = None, relational_only: bool = False,
                  want_sel: bool = True, share_prefix: bool = True, multipass_compact: bool = False,
-                 full_last_layer: bool = False):
+                 full_last_layer: bool = False, kv_dtype: str = "f16", sample_u=None):
+        if kv_dtype not in ("f16", "i8"):
+            raise ValueError(kv_dtype)
         self.device = torch.device(device)
         self.query = query
         self.dm = dmodel if dmodel is not None else DeviceModel(model, device)
         self.probe = DeviceTable(tables["probe"], device)
         self.build = DeviceTable(tables["build"], device, with_list=False) if tables.get("build") is not None else None
         self.q = make_query(query, self.probe, self.build, tables.get("prefix", ()))
+        if sample_u is not None:
+            u = torch.as_tensor(sample_u, dtype=torch.float32).to(self.device).contiguous()
+            if u.shape != (self.probe.n_rows, self.q.gen_tokens):
+                raise ValueError(f"sample_u: [{self.probe.n_rows}, {self.q.gen_tokens}] wanted, got {tuple(u.shape)}")
+            self.sample_u = u
+            self.q.sample_u = _ptr(u)
         opts = B.aiq_plan_opts()
+        opts.kv_dtype = B.AIQ_I8 if kv_dtype == "i8" else 0
         opts.chunk_tokens = int(chunk_tokens)
         opts.n_layers_override = _layers_opt(n_layers)
         opts.flags = (B.AIQ_PLAN_RELATIONAL_ONLY if relational_only else 0) | \

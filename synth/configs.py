@@ -140,6 +140,7 @@ class Query:
     like: Tuple[int, ...] = ()        # LIKE '%pattern%' over the generated token ids
     pair_key: Optional[str] = None    # Q4: classify pairs of selected rows with equal keys in this column
     max_pairs: int = 0                # Q4: capacity for candidate pairs
+    sampling: Optional[Tuple[float, int, float, float]] = None   # AI_TRANSFORM: temperature, top_k, top_p, min_p
 
 
 @dataclass(frozen=True)

@@ -8,6 +8,7 @@ import torch
 
 from paper_2608_10139_amd import binding as B
 from paper_2608_10139_amd.device import DeviceKvCache, sample
+from tests.test_abi_host import model, query, table
 
 FAKE = 0x10000
 
@@ -147,3 +148,39 @@ def test_wrapper_refusals():
     for args in ((x, x[:, 0]), (x[0], x[0]), (x.double(), x[:, 0])):
         with pytest.raises(ValueError):
             sample(*args)
+
+
+def gen_query(**kw):
+    q = query(gen_tokens=4, eos_id=-1)
+    for k, v in kw.items():
+        if k in ("temperature", "top_k", "top_p", "min_p"):
+            setattr(q.sampling, k, v)
+        else:
+            setattr(q, k, v)
+    return q
+
+
+def plan(q, **opts):
+    o = B.aiq_plan_opts()
+    for k, v in opts.items():
+        setattr(o, k, v)
+    return B.aiq_plan_create_status(model(), table(), None, q, o)
+
+
+GOOD = dict(sample=1, temperature=1.0, top_p=1.0, sample_u=FAKE)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(), B.AIQ_OK), (dict(temperature=0.0, sample_u=0), B.AIQ_OK), (dict(top_k=5, top_p=0.5, min_p=0.5), B.AIQ_OK),
+    (dict(sample=2), B.AIQ_EINVAL), (dict(sample_u=0), B.AIQ_EINVAL), (dict(sample_u=FAKE + 2), B.AIQ_EINVAL),
+    (dict(temperature=-1.0), B.AIQ_EINVAL), (dict(top_p=0.0), B.AIQ_EINVAL), (dict(min_p=2.0), B.AIQ_EINVAL),
+    (dict(top_k=-1), B.AIQ_EINVAL), (dict(gen_tokens=0), B.AIQ_EINVAL)], ids=str)
+def test_sampling_queries(kw, code):
+    assert plan(gen_query(**{**GOOD, **kw})) == code
+
+
+def test_cache_types_of_a_plan():
+    assert plan(gen_query(), kv_dtype=B.AIQ_I8) == plan(gen_query(), kv_dtype=B.AIQ_F16) == plan(gen_query()) == B.AIQ_OK
+    assert plan(gen_query(), kv_dtype=B.AIQ_BF16) == plan(gen_query(), kv_dtype=-1) == B.AIQ_EINVAL
+    assert plan(query(), kv_dtype=B.AIQ_I8) == B.AIQ_EINVAL   # nothing is generated
+    assert plan(query(), kv_dtype=B.AIQ_F16) == B.AIQ_OK
