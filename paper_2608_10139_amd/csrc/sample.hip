@@ -2,51 +2,102 @@
 // AI_TRANSFORM): temperature, top-k, top-p, min-p, inverse distribution in the
 // order of ids.
 //
-// A workgroup per row.  Weights are whole numbers, round(2^S exp((x - m) / T)) from fp64
-// exponentials, S such that a whole vocabulary's sum fits 63 bits: sums do not depend on
-// their order, so they may come from LDS atomics, and a weight keeps 2^-47 of the
-// largest at 32,000 tokens.  All three filters keep a prefix of the tokens in
-// descending order of logits, so the kept set is a threshold: the prefix's last
-// value and, where only some of the tokens equal to it belong, the last id of
-// those.  It is found digit by digit of the value's ordered bit pattern, counting
-// tokens (top-k) or adding weights (top-p) per digit.
+// A workgroup of 16 waves per row, each wave a run of ids; every pass reads the row again,
+// from the L2 (held in registers, 32 logits per thread, it left none for the passes
+// to overlap: 580 us for 4,096 rows of 32,000 against 465).
+//
+// Weights are whole numbers, round(2^S exp((x - m) / T)) from fp64 exponentials
+// (below), S such that a whole vocabulary's sum fits 62 bits: sums do not
+// depend on their order, so they may come from LDS atomics, and a weight keeps
+// 2^-47 of the largest at 32,000 tokens.  (In 32 bits a border between two tokens
+// moves by 1e-7 of the sum, which is a share of 3e-3 of all random numbers with
+// 32,000 borders; here it is below 1e-8.)
+//
+// All filters keep a prefix of the tokens in descending order, equal ones by
+// ascending id, so the kept set is a threshold (x, id).  Top-k and top-p find theirs
+// the same way, by counts or by weights: a histogram over the distance to the
+// maximum (2,048 bins in LDS), the bin in which the count or the sum reaches its
+// target, and in that bin the token itself, by comparing its tokens (60 or so) with each other.
+// A bin with more than CAP tokens (equal logits, a far outlier) is halved bit by bit instead.
 #include "aiq_internal.h"
 #include "dev_util.h"
 
+#include <type_traits>
+
 namespace aiq {
 
-constexpr int SN = 1024;              // threads
-constexpr int SW = SN / 64;           // waves
+constexpr int SW_MAX = 16;            // waves
 constexpr int BINS = 2048;
+// tokens that a workgroup of SW waves gathers and compares with each other (LDS for four small ones on a CU)
+constexpr int cap(int sw) { return sw == 16 ? 2048 : 1024; }
 
 template <int DT>
-__device__ __forceinline__ float logit(const void* p, int64_t i) {
-  if (DT == AIQ_F32) return static_cast<const float*>(p)[i];
-  const uint16_t v = static_cast<const uint16_t*>(p)[i];
-  return DT == AIQ_F16 ? h2f(v) : bf2f(v);
+struct Logits4 {   // 4 logits, aligned to one
+  typedef float T;
+  T v[4];
+} __attribute__((packed, aligned(4)));
+template <>
+struct Logits4<AIQ_F16> {
+  typedef uint16_t T;
+  T v[4];
+} __attribute__((packed, aligned(2)));
+template <>
+struct Logits4<AIQ_BF16> {
+  typedef uint16_t T;
+  T v[4];
+} __attribute__((packed, aligned(2)));
+
+template <int DT>
+__device__ __forceinline__ float to_logit(typename Logits4<DT>::T v) {   // NaN: never taken
+  float x;
+  if constexpr (DT == AIQ_F32)
+    x = v;
+  else
+    x = DT == AIQ_F16 ? h2f(v) : bf2f(v);
+  return fmaxf(x, -INFINITY);
 }
 
-// Bit pattern that orders as the values (0 for NaN: below -infinity; -0 as 0)
+// Bit pattern that orders as the values do (-0 as 0)
 __device__ __forceinline__ uint32_t order_key(float x) {
-  if (x != x) return 0;
   const uint32_t b = __float_as_uint(x == 0.f ? 0.f : x);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-constexpr uint32_t KEY_NEG_INF = 0x007FFFFFu;   // order_key(-infinity)
 
+constexpr double ROUND = 0x1.8p52;   // x + ROUND: x rounded to a whole number, in the low bits
 struct Weigh {
-  double inv_t, up, min_p;
+  double c;         // log2(e) / T
+  double d0;        // a distance whose weight rounds to 0
+  double least;     // min_p * 2^S
+  int s;            // S
   float m;
-  // exp((x - m) / T); 1 at the maximum (an infinite one too), 0 for NaN and -infinity
-  __device__ __forceinline__ double exp_of(float x) const {
-    if (x == m) return 1.0;
-    const double z = (static_cast<double>(x) - static_cast<double>(m)) * inv_t;
-    return z > -700.0 ? exp(z) : 0.0;   // false for NaN
+  // 2^S exp((x - m) / T), not rounded yet: 2^y = 2^n 2^f with n the nearest whole
+  // number and 2^f on [-1/2, 1/2] as 1 + f Q(f), Q of degree 8 through the
+  // Chebyshev nodes (relative error 4e-14); exactly 2^S at the maximum.
+  __device__ __forceinline__ double real(float x) const {
+    const double d = fmax(static_cast<double>(x) - static_cast<double>(m), d0);
+    const double t = fma(d, c, ROUND), f = fma(d, c, ROUND - t);
+    double q = 0x1.b638809761cfdp-24;
+    q = fma(q, f, 0x1.63d13636b876dp-20);
+    q = fma(q, f, 0x1.ffcb9515b4237p-17);
+    q = fma(q, f, 0x1.4308ac85aa3bbp-13);
+    q = fma(q, f, 0x1.5d87fe86fe84cp-10);
+    q = fma(q, f, 0x1.3b2ab7181b759p-7);
+    q = fma(q, f, 0x1.c6b08d7047e52p-5);
+    q = fma(q, f, 0x1.ebfbdff823cedp-3);
+    q = fma(q, f, 0x1.62e42fefa39efp-1);
+    const int64_t z = __double_as_longlong(fma(q, f, 1.0));   // times 2^(n + S), in the exponent's bits
+    const uint32_t n = static_cast<uint32_t>(__double_as_longlong(t)) + s;
+    return __longlong_as_double(z + (static_cast<int64_t>(n << 20) << 32));
   }
-  __device__ __forceinline__ uint64_t of(float x) const { return static_cast<uint64_t>(exp_of(x) * up + 0.5); }
+  // the nearest whole number of a value below 2^51, with BIAS added
+  static __device__ __forceinline__ uint64_t biased(double v) {
+    return static_cast<uint64_t>(__double_as_longlong(v + 0x1p52));
+  }
+  static constexpr uint64_t BIAS = 0x433ull << 52;
+  __device__ __forceinline__ uint64_t of(float x) const { return biased(real(x)) - BIAS; }
   __device__ __forceinline__ uint64_t kept(float x) const {   // 0 below min_p
-    const double e = exp_of(x);
-    return e >= min_p ? static_cast<uint64_t>(e * up + 0.5) : 0;
+    const double v = real(x);
+    return v >= least ? biased(v) - BIAS : 0;
   }
 };
 
@@ -54,33 +105,47 @@ __device__ __forceinline__ uint64_t shfl_u64(uint64_t v, int mask) {
   const uint32_t lo = __shfl_xor(static_cast<uint32_t>(v), mask), hi = __shfl_xor(static_cast<uint32_t>(v >> 32), mask);
   return (static_cast<uint64_t>(hi) << 32) | lo;
 }
-__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += shfl_u64(v, o);
-  return v;
+// v shifted or broadcast between lanes (0 where nothing comes), added
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp_add_u64(uint64_t v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(v)), CTRL, ROWS, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(static_cast<uint32_t>(v >> 32)), CTRL, ROWS, 0xF, true);
+  return v + ((static_cast<uint64_t>(hi) << 32) | lo);
 }
-// inclusive sum over the lanes up to this one
-__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t lo = __shfl_up(static_cast<uint32_t>(v), o), hi = __shfl_up(static_cast<uint32_t>(v >> 32), o);
-    if (lane >= o) v += (static_cast<uint64_t>(hi) << 32) | lo;
-  }
-  return v;
+// inclusive sum over the lanes up to this one: inside rows of 16 (row_shr 1, 2, 4, 8), then the last
+// lane of a row to the next row, of a half to the other (row_bcast 15, 31)
+__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v) {
+  v = dpp_add_u64<0x111, 0xF>(v);
+  v = dpp_add_u64<0x112, 0xF>(v);
+  v = dpp_add_u64<0x114, 0xF>(v);
+  v = dpp_add_u64<0x118, 0xF>(v);
+  v = dpp_add_u64<0x142, 0xA>(v);
+  return dpp_add_u64<0x143, 0xC>(v);
 }
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(v)), 63);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(v >> 32)), 63);
+  return (static_cast<uint64_t>(hi) << 32) | lo;
+}
+__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) { return last_lane(wave_scan_u64(v)); }
 
-struct SampleLds {
-  uint32_t cnt[BINS];
-  uint64_t mass[BINS];
-  uint64_t wave[SW];
-  uint64_t before;
-  uint32_t key, ties;
-  int32_t id;
-  uint32_t best;
+struct SampleSums {
+  uint64_t wave[SW_MAX];
+  float lo[SW_MAX];
+};
+template <int SW>
+struct SampleLds : SampleSums {
+  static constexpr int CAP = cap(SW);
+  uint64_t bin[BINS];
+  uint64_t key[CAP];     // gathered tokens: (ordered bits of the logit, ~id)
+  uint64_t w[CAP];
+  uint64_t before, target;
+  int32_t at, n;         // the bin, its tokens
+  uint64_t last;         // the threshold, as a key
 };
 
-// Sum of v over the workgroup, in every thread.
-__device__ __forceinline__ uint64_t block_sum(uint64_t v, SampleLds& s) {
+template <int SW>
+__device__ __forceinline__ uint64_t block_sum(uint64_t v, SampleSums& s) {
   v = wave_sum_u64(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = v;
@@ -91,213 +156,550 @@ __device__ __forceinline__ uint64_t block_sum(uint64_t v, SampleLds& s) {
   return t;
 }
 
-// The first token, in descending order, at which the count (MASS: the sum of
-// weights) of the tokens so far reaches `target` (>= 1, at most all of it): its key
-// in s.key and how many of the tokens with that key that takes in s.ties, the
-// weights of those above the key in s.before.
-template <int DT, bool MASS>
-__device__ void find_prefix(const void* row, int V, const Weigh& w, uint64_t target, SampleLds& s) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  uint32_t prefix = 0, mask = 0;
-  uint64_t count_above = 0, mass_above = 0;
-  for (int level = 0; level < 3; ++level) {
-    const int shift = level == 0 ? 21 : level == 1 ? 10 : 0;
-    const int bins = level == 2 ? 1024 : 2048;
-    for (int b = tid; b < BINS; b += SN) {
-      s.cnt[b] = 0;
-      s.mass[b] = 0;
+// A workgroup's row: f(logit, id) for every one of this thread's tokens, in
+// ascending order of ids (-infinity past the end); all lanes call f together.
+template <int DT>
+struct Row {
+  const typename Logits4<DT>::T* p;
+  int V, rounds, id0;   // this thread's tokens: id0 + 256 * round + 0 .. 3
+  bool inf;             // the maximum is +infinity: its tokens read as 0, the others as -infinity
+  __device__ __forceinline__ void load4(int it, float (&v)[4]) const {
+    const int id = id0 + it * 256;
+    if (__builtin_amdgcn_readfirstlane(id) + 256 <= V) {   // all of the wave's
+      const Logits4<DT> y = *reinterpret_cast<const Logits4<DT>*>(p + id);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = to_logit<DT>(y.v[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = id + e < V ? to_logit<DT>(p[id + e]) : -INFINITY;
     }
-    __syncthreads();
-  #pragma unroll 2
-    for (int i = tid; i < V; i += SN) {
-      const float x = logit<DT>(row, i);
-      const uint32_t k = order_key(x);
-      if (k <= KEY_NEG_INF || (k & mask) != prefix) continue;
-      const int b = (k >> shift) & (bins - 1);
-      atomicAdd(&s.cnt[b], 1u);
-      atomicAdd(reinterpret_cast<unsigned long long*>(&s.mass[b]), static_cast<unsigned long long>(w.of(x)));
+    if (inf) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = v[e] == INFINITY ? 0.f : -INFINITY;
     }
-    __syncthreads();
-    // from the top: one wave, 64 runs of bins / 64 bins
-    if (tid < 64) {
-      const int per = bins / 64, top = bins - 1 - lane * per;
-      uint64_t c = 0, ms = 0;
-      for (int q = 0; q < per; ++q) {
-        c += s.cnt[top - q];
-        ms += s.mass[top - q];
-      }
-      const uint64_t ci = wave_scan_u64(c, lane), mi = wave_scan_u64(ms, lane);
-      const uint64_t done = MASS ? mass_above + mi : count_above + ci;
-      const uint64_t hit = __ballot(done >= target);
-      if (hit && lane == __builtin_ctzll(hit)) {
-        uint64_t ca = count_above + ci - c, ma = mass_above + mi - ms;
-        int b = top;
-        for (; b > top - per + 1; --b) {
-          if ((MASS ? ma + s.mass[b] : ca + s.cnt[b]) >= target) break;
-          ca += s.cnt[b];
-          ma += s.mass[b];
-        }
-        s.key = prefix | (static_cast<uint32_t>(b) << shift);
-        s.before = ma;
-        s.wave[0] = ca;
-        s.wave[1] = s.mass[b];
-        s.wave[2] = s.cnt[b];
-      }
-    }
-    __syncthreads();
-    prefix = s.key;
-    mask = shift ? ~((1u << shift) - 1u) : ~0u;
-    mass_above = s.before;
-    count_above = s.wave[0];
-    if (level == 2 && tid == 0) {
-      const uint64_t each = s.wave[1] / s.wave[2];   // equal logits, equal weights
-      s.ties = static_cast<uint32_t>(MASS ? (target - mass_above + each - 1) / each : target - count_above);
-    }
-    __syncthreads();
   }
+  template <typename F>
+  __device__ __forceinline__ void each4(F f) const {   // f(4 logits, first id)
+    float v[4];
+    load4(0, v);
+#pragma unroll 1
+    for (int it = 0; it < rounds; ++it) {
+      float next[4];
+      load4(it + 1 < rounds ? it + 1 : it, next);   // in flight while this round is worked on
+      f(v, id0 + it * 256);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = next[e];
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    each4([&](const float (&v)[4], int id) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(v[e], id + e);
+    });
+  }
+};
+
+// tokens up to the threshold (xt, idt), the tokens kept so far
+__device__ __forceinline__ bool upto(float x, int id, float xt, int idt) {
+  return x > xt || (x == xt && id <= idt);
+}
+__device__ __forceinline__ uint64_t token_key(float x, int id) {   // larger is earlier
+  return (static_cast<uint64_t>(order_key(x)) << 32) | static_cast<uint32_t>(~id);
+}
+__device__ __forceinline__ float key_logit(uint64_t key) {
+  const uint32_t k = static_cast<uint32_t>(key >> 32);
+  return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+__device__ __forceinline__ int key_id(uint64_t key) { return static_cast<int>(~static_cast<uint32_t>(key)); }
+
+// Bins of the distance to the maximum: `span` over all but the last, which takes what is beyond
+struct Bins {
+  float m, per;
+  __device__ __forceinline__ Bins(float m_, float span) : m(m_), per(span > 0.f ? static_cast<float>(BINS - 1) / span : 0.f) {}
+  __device__ __forceinline__ float place(float x) const { return fminf((m - x) * per, static_cast<float>(BINS - 1)); }
+};
+
+// The bin in which the counts or weights in `bin` (of all threads) reach the target that goal(total)
+// gives: s.at, with s.before ahead of it.  Ends with a barrier.
+template <int SW, typename T, typename G>
+__device__ __forceinline__ void cross(const T* bin, G goal, SampleLds<SW>& s) {
+  constexpr int PB = BINS / (64 * SW);
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  uint64_t mine = 0;
+  for (int q = 0; q < PB; ++q) mine += bin[PB * tid + q];
+  const uint64_t incl = wave_scan_u64(mine);
+  if (lane == 63) s.wave[wv] = incl;
+  __syncthreads();
+  uint64_t before = incl - mine, total = 0;
+#pragma unroll
+  for (int x = 0; x < SW; ++x) {
+    if (x < wv) before += s.wave[x];
+    total += s.wave[x];
+  }
+  const uint64_t target = goal(total);
+  if (before < target && target <= before + mine) {
+    int q = 0;
+    for (; q < PB - 1 && before + bin[PB * tid + q] < target; ++q) before += bin[PB * tid + q];
+    s.at = PB * tid + q;
+    s.before = before;
+    s.target = target;
+  }
+  __syncthreads();
 }
 
-template <int DT>
-__global__ __launch_bounds__(SN) void k_sample(SampleArgs a) {
-  __shared__ SampleLds s;
+// Gathers the tokens that pred picks: s.n of them, the first CAP as keys.  All lanes together.
+template <int SW>
+__device__ __forceinline__ void gather(bool in, float x, int id, SampleLds<SW>& s) {
+  const uint64_t b = __ballot(in);
+  if (!b) return;
+  const int lead = __builtin_ctzll(b);
+  int slot = 0;
+  if ((threadIdx.x & 63) == lead) slot = atomicAdd(&s.n, __popcll(b));
+  slot = __shfl(slot, lead) + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(b >> 32),
+                                                       __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(b), 0));
+  if (in && slot < s.CAP) s.key[slot] = token_key(x, id);
+}
+
+// p_of top_p of a sum of weights, as a whole number in 1 .. total
+__device__ __forceinline__ uint64_t share_of(double p, uint64_t total) {
+  const double t = ceil(p * static_cast<double>(total));
+  const uint64_t g = t < static_cast<double>(total) ? static_cast<uint64_t>(t) : total;
+  return g ? g : 1;
+}
+
+// Moves the threshold (xt, idt) to the token at which the count (MASS: the sum of weights) of the
+// tokens reaches its target: top_k, or top_p of the sum of the tokens kept so far.
+template <int DT, int SW, bool MASS>
+__device__ __forceinline__ void find(const Row<DT>& row, const Weigh& w, double top, float span, float& xt, int& idt, SampleLds<SW>& s) {
+  constexpr int SN = 64 * SW, CAP = cap(SW);
+  const int tid = threadIdx.x, lane = tid & 63;
+  typedef std::conditional_t<MASS, uint64_t, uint32_t> T;
+  T* bin = reinterpret_cast<T*>(s.bin);
+  const Bins bins(w.m, span);
+  for (int b = tid; b < BINS; b += SN) bin[b] = 0;
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  T rest = 0;   // the last bin's
+  row.each4([&](const float (&x)[4], int id) {
+    bool in[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) in[e] = upto(x[e], id + e, xt, idt);
+    if (!__any(in[0] || in[1] || in[2] || in[3])) return;
+    T v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (MASS)
+        v[e] = w.of(x[e]);
+      else
+        v[e] = 1;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int b = static_cast<int>(bins.place(x[e]));
+      if (in[e] && b == BINS - 1) rest += v[e];
+      if (in[e] && b < BINS - 1) atomicAdd(reinterpret_cast<std::conditional_t<MASS, unsigned long long, uint32_t>*>(&bin[b]), v[e]);
+    }
+  });
+  const uint64_t all = wave_sum_u64(rest);
+  if (lane == 0 && all)
+    atomicAdd(reinterpret_cast<std::conditional_t<MASS, unsigned long long, uint32_t>*>(&bin[BINS - 1]), static_cast<T>(all));
+  __syncthreads();
+  cross<SW>(bin, [&](uint64_t total) -> uint64_t {
+    return MASS ? share_of(top, total) : top < static_cast<double>(total) ? static_cast<uint64_t>(top) : total;
+  }, s);
+  const int at = s.at;
+  const uint64_t before = s.before, target = s.target;
+  const float from = static_cast<float>(at), to = at == BINS - 1 ? INFINITY : static_cast<float>(at + 1);
+  auto in_bin = [&](float x, int id) {
+    const float f = bins.place(x);
+    return f >= from && f < to && upto(x, id, xt, idt);
+  };
+  row.each4([&](const float (&x)[4], int id) {
+    bool in[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) in[e] = in_bin(x[e], id + e);
+    if (!__any(in[0] || in[1] || in[2] || in[3])) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) gather(in[e], x[e], id + e, s);
+  });
+  __syncthreads();
+  const int n = s.n;
+  if (n <= CAP) {
+    for (int i = tid; MASS && i < n; i += SN) s.w[i] = w.of(key_logit(s.key[i]));
+    __syncthreads();
+    int each = 64;   // threads per token
+    while (each > 1 && n * each > SN) each >>= 1;
+    for (int i0 = 0; i0 < n; i0 += SN / each) {
+      const int i = i0 + tid / each;
+      const uint64_t key = i < n ? s.key[i] : 0;
+      uint64_t ahead = 0;   // of the bin's tokens ahead of this one
+      for (int j = tid % each; j < n; j += each)
+        if (s.key[j] > key) ahead += MASS ? s.w[j] : 1;
+      for (int o = each / 2; o > 0; o >>= 1) ahead += shfl_u64(ahead, o);
+      ahead += before;
+      if (i < n && tid % each == 0 && ahead < target && target <= ahead + (MASS ? s.w[i] : 1)) s.last = key;
+    }
+  } else {
+    // the largest key K such that the bin's tokens with keys from K on reach the target, bit by bit
+    uint32_t K = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t k = K | (1u << bit);
+      uint64_t v = 0;
+      row.each([&](float x, int id) {
+        if (in_bin(x, id) && order_key(x) >= k) v += MASS ? w.of(x) : 1;
+      });
+      if (before + block_sum<SW>(v, s) >= target) K = k;
+    }
+    uint64_t above = 0;
+    row.each([&](float x, int id) {
+      if (in_bin(x, id) && order_key(x) > K) above += MASS ? w.of(x) : 1;
+    });
+    above = before + block_sum<SW>(above, s);
+    // of the tokens with that key the first `t` ids do not reach it, the largest such t
+    int t = 0;
+    for (int bit = 24; bit >= 0; --bit) {
+      uint64_t v = 0;
+      const int u = t | (1 << bit);
+      row.each([&](float x, int id) {
+        if (id < u && in_bin(x, id) && order_key(x) == K) v += MASS ? w.of(x) : 1;
+      });
+      if (above + block_sum<SW>(v, s) < target) t = u;
+    }
+    if (tid == 0) s.last = (static_cast<uint64_t>(K) << 32) | static_cast<uint32_t>(~t);
+  }
+  __syncthreads();
+  xt = key_logit(s.last);
+  idt = key_id(s.last);
+  __syncthreads();
+}
+
+// The sum of weights, in the order of ids, that the drawn token is the first to exceed
+__device__ __forceinline__ uint64_t draw_target(float u, uint64_t total) {
+  if (!(u < 1.f)) return total - 1;
+  const double t = static_cast<double>(u) * static_cast<double>(total);
+  const uint64_t g = t > 0.0 ? static_cast<uint64_t>(t) : 0;
+  return g < total ? g : total - 1;
+}
+
+// Sorts the first `n2` (a power of two) keys, the largest first.
+template <int SW>
+__device__ __forceinline__ void sort_keys(uint64_t* key, int n2) {
+  for (int k = 2; k <= n2; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      for (int i = threadIdx.x; i < n2 / 2; i += 64 * SW) {
+        const int a = 2 * i - (i & (j - 1)), b = a + j;   // i's pair at distance j
+        const uint64_t x = key[a], y = key[b];
+        if ((a & k) == 0 ? x < y : x > y) {
+          key[a] = y;
+          key[b] = x;
+        }
+      }
+      __syncthreads();
+    }
+}
+
+// Top-k with what follows it among few tokens: of the 4 maxima that each thread has (of every fourth of its
+// tokens), k lie in the bins up to one, and so at least k tokens do; where they are no more than CAP, the filters and the
+// draw need these alone, sorted.  False: they are more (or fewer maxima than k).
+template <int DT, int SW>
+__device__ __forceinline__ bool draw_few(const Row<DT>& row, const Weigh& w, const float (&most)[4], const SampleArgs& a,
+                                         int64_t r, float u, SampleLds<SW>& s) {
+  constexpr int SN = 64 * SW, CAP = cap(SW), PER = CAP / SN > 0 ? CAP / SN : 1;   // sorted tokens per thread
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  uint32_t* bin = reinterpret_cast<uint32_t*>(s.bin);
+  const Bins bins(w.m, 32.f);
+  for (int b = tid; b < BINS; b += SN) bin[b] = 0;
+  if (tid == 0) {
+    s.n = 0;
+    s.at = -1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (most[q] > -INFINITY) atomicAdd(&bin[static_cast<int>(bins.place(most[q]))], 1u);
+  __syncthreads();
+  cross<SW>(bin, [&](uint64_t total) { return static_cast<uint64_t>(a.top_k); }, s);
+  const int at = s.at;
+  if (at < 0 || at == BINS - 1) return false;
+  const float to = static_cast<float>(at + 1);
+  row.each4([&](const float (&x)[4], int id) {
+    bool in[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) in[e] = (w.m - x[e]) * bins.per < to;
+    if (!__any(in[0] || in[1] || in[2] || in[3])) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) gather(in[e], x[e], id + e, s);
+  });
+  __syncthreads();
+  const int n = s.n;
+  if (n > CAP) return false;
+  const int k = a.top_k < n ? a.top_k : n;
+  if (n <= 128) {   // by comparing all with all, SN / 128 threads or more per token: no sort's chain of steps
+    const int each = SN / (n <= 64 ? 64 : 128), i = tid / each;
+    for (int j = tid; j < n; j += SN) s.w[j] = w.of(key_logit(s.key[j]));
+    __syncthreads();
+    const uint64_t key = i < n ? s.key[i] : 0, mine = i < n ? s.w[i] : 0;
+    uint64_t ahead = 0;
+    int rank = 0;
+    for (int j = tid % each; j < n; j += each)
+      if (s.key[j] > key) {
+        ahead += s.w[j];
+        ++rank;
+      }
+    for (int o = each / 2; o > 0; o >>= 1) {
+      ahead += shfl_u64(ahead, o);
+      rank += __shfl_xor(rank, o);
+    }
+    const bool lead = i < n && tid % each == 0;
+    uint64_t total = block_sum<SW>(lead && rank < k ? mine : 0, s);
+    const uint64_t target = a.top_p < 1.0 ? share_of(a.top_p, total) : total;
+    const uint64_t keep = i < n && rank < k && ahead < target ? w.kept(key_logit(key)) : 0;
+    if (lead) s.w[i] = keep;
+    total = block_sum<SW>(lead ? keep : 0, s);
+    const uint64_t goal = draw_target(u, total);
+    uint64_t below = 0;   // kept weights of lower ids: larger low words
+    for (int j = tid % each; j < n; j += each)
+      if (static_cast<uint32_t>(s.key[j]) > static_cast<uint32_t>(key)) below += s.w[j];
+    for (int o = each / 2; o > 0; o >>= 1) below += shfl_u64(below, o);
+    if (lead && below <= goal && goal < below + keep) a.token[r] = key_id(key);
+    __syncthreads();
+    return true;
+  }
+  int n2 = 256;
+  while (n2 < n) n2 <<= 1;
+  for (int i = n + tid; i < n2; i += SN) s.key[i] = 0;
+  __syncthreads();
+  sort_keys<SW>(s.key, n2);
+  // weights in order, and their running sums
+  uint64_t v[PER], mine = 0;
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int i = tid * PER + q;
+    v[q] = i < k ? w.of(key_logit(s.key[i])) : 0;
+    mine += v[q];
+  }
+  auto scan = [&](uint64_t x, uint64_t& total) {   // of the threads before this one
+    const uint64_t incl = wave_scan_u64(x);
+    __syncthreads();
+    if (lane == 63) s.wave[wv] = incl;
+    __syncthreads();
+    uint64_t before = incl - x;
+    total = 0;
+#pragma unroll
+    for (int y = 0; y < SW; ++y) {
+      if (y < wv) before += s.wave[y];
+      total += s.wave[y];
+    }
+    return before;
+  };
+  uint64_t total;
+  uint64_t ahead = scan(mine, total);
+  const uint64_t target = a.top_p < 1.0 ? share_of(a.top_p, total) : total;
+  uint64_t keep[PER], id_key[PER];
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {   // kept: those before the sum reaches the target
+    const int i = tid * PER + q;
+    const bool in = i < k && ahead < target;
+    keep[q] = in ? w.kept(key_logit(s.key[i])) : 0;
+    id_key[q] = in ? (s.key[i] << 32) | static_cast<uint32_t>(i) : 0;   // (~id, place): the lowest id is the largest
+    ahead += v[q];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int i = tid * PER + q;
+    if (i >= n2) break;
+    s.key[i] = id_key[q];
+    s.w[i] = keep[q];
+  }
+  __syncthreads();
+  sort_keys<SW>(s.key, n2);
+  mine = 0;
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    const int i = tid * PER + q;
+    v[q] = i < n2 && s.key[i] ? s.w[static_cast<uint32_t>(s.key[i])] : 0;
+    mine += v[q];
+  }
+  ahead = scan(mine, total);
+  const uint64_t goal = draw_target(u, total);
+#pragma unroll
+  for (int q = 0; q < PER; ++q) {
+    if (ahead <= goal && goal < ahead + v[q]) a.token[r] = key_id(s.key[tid * PER + q] >> 32);
+    ahead += v[q];
+  }
+  __syncthreads();
+  return true;
+}
+
+template <int DT, int SW, bool FILTER>
+__global__ __launch_bounds__(64 * SW, SW == SW_MAX || FILTER ? 4 : 8) void k_sample(SampleArgs a) {
+  constexpr int SN = 64 * SW;
+  __shared__ std::conditional_t<FILTER, SampleLds<SW>, SampleSums> s;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int V = a.vocab;
   int64_t rows = a.n_rows;
   if (a.n_ptr && *a.n_ptr < rows) rows = *a.n_ptr;
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const char* row = static_cast<const char*>(a.logits) + r * a.ld * (DT == AIQ_F32 ? 4 : 2);
-    // the maximum, and the lowest id that has it
-    uint64_t best = 0;   // (key, ~id)
-    for (int i = tid; i < V; i += SN) {
-      const uint64_t k = (static_cast<uint64_t>(order_key(logit<DT>(row, i))) << 32) | static_cast<uint32_t>(~i);
-      best = k > best ? k : best;
+    Row<DT> row;
+    row.p = static_cast<const typename Logits4<DT>::T*>(a.logits) + r * a.ld;
+    row.V = V;
+    row.rounds = (V + SN * 4 - 1) / (SN * 4);
+    const int run = row.rounds * 256;   // ids per wave
+    row.id0 = wv * run + lane * 4;
+    row.inf = false;
+    // the maximum and the least finite logit; at temperature 0 the lowest id that has the maximum
+    float best = -INFINITY, least = INFINITY;
+    const bool greedy = a.temperature == 0.0;
+    int first = INT32_MAX;
+    float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};   // of every fourth of the thread's tokens
+    if (greedy)
+      row.each([&](float x, int id) {
+        first = x > best ? id : first;
+        best = fmaxf(best, x);
+      });
+    else {
+      row.each4([&](const float (&v)[4], int id) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          most[e] = fmaxf(most[e], v[e]);
+          if (FILTER) least = v[e] > -INFINITY ? fminf(least, v[e]) : least;
+        }
+      });
+      best = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
     }
+    uint64_t top = (static_cast<uint64_t>(order_key(best)) << 32) | static_cast<uint32_t>(~first);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
-      const uint64_t y = shfl_u64(best, o);
-      best = y > best ? y : best;
+      const uint64_t y = shfl_u64(top, o);
+      top = y > top ? y : top;
+      least = fminf(least, __shfl_xor(least, o));
     }
-    __syncthreads();
-    if (lane == 0) s.wave[wv] = best;
+    __syncthreads();   // (the row before)
+    if (lane == 0) {
+      s.wave[wv] = top;
+      s.lo[wv] = least;
+    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < SW; ++w) best = s.wave[w] > best ? s.wave[w] : best;
-    __syncthreads();
-    const uint32_t mk = static_cast<uint32_t>(best >> 32);
-    const int first = static_cast<int>(~static_cast<uint32_t>(best));
-    if (mk <= KEY_NEG_INF || a.temperature == 0.0) {
-      if (tid == 0) a.token[r] = mk <= KEY_NEG_INF ? 0 : first;
-      continue;
+    for (int x = 0; x < SW; ++x) {
+      top = s.wave[x] > top ? s.wave[x] : top;
+      least = fminf(least, s.lo[x]);
     }
+    __syncthreads();
+    const uint32_t mk = static_cast<uint32_t>(top >> 32);
     Weigh w;
     w.m = __uint_as_float(mk & 0x80000000u ? mk & 0x7FFFFFFFu : ~mk);
-    w.inv_t = 1.0 / a.temperature;
-    w.min_p = a.min_p;
-    w.up = static_cast<double>(1ull << (62 - (32 - __builtin_clz(static_cast<uint32_t>(V)))));
-    // the kept prefix: keys above `key`, and those equal to it up to id `last`
-    uint32_t key = KEY_NEG_INF + 1;
-    int last = V;
-    uint32_t ties = 0;   // 0: all tokens equal to the key
-    if (a.top_k > 0) {
-      // fewer finite tokens than top_k: all of them
-      uint32_t c = 0;
-      for (int i = tid; i < V; i += SN) c += order_key(logit<DT>(row, i)) > KEY_NEG_INF;
-      const uint64_t n = block_sum(c, s);
-      if (n > static_cast<uint64_t>(a.top_k)) {
-        find_prefix<DT, false>(row, V, w, a.top_k, s);
-        key = s.key;
-        ties = s.ties;
-        __syncthreads();
-      }
+    if (w.m == -INFINITY || greedy) {
+      if (tid == 0) a.token[r] = w.m == -INFINITY ? 0 : static_cast<int>(~static_cast<uint32_t>(top));
+      continue;
     }
+    if (w.m == INFINITY) {
+      row.inf = true;
+      w.m = least = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) most[q] = most[q] == INFINITY ? 0.f : -INFINITY;
+    }
+    const int bits = 32 - __builtin_clz(static_cast<uint32_t>(V));
+    w.c = 1.4426950408889634 * fmin(1.0 / a.temperature, 1e300);
+    w.s = bits > 12 ? 62 - bits : 50;
+    w.d0 = fmax(-(w.s + 4.0) / w.c, -1e300);
+    w.least = a.min_p * static_cast<double>(1ull << w.s);
+    float xt = -INFINITY;   // all but -infinity
+    int idt = -1;
+    const float range = w.m - least;
+    const float u = a.u[a.u_row ? a.u_row[*a.u_base + a.u_add + r] * a.u_ld + a.u_at : r];
+    if constexpr (FILTER) {
+    if (a.top_k > 0 && draw_few<DT, SW>(row, w, most, a, r, u, s)) continue;
+    if (a.top_k > 0) find<DT, SW, false>(row, w, a.top_k, fminf(range, 40.f), xt, idt, s);
     if (a.top_p < 1.0) {
-      // the mass of the first n_k: keys above, and `ties` of the equal ones
-      uint64_t above = 0;
-      for (int i = tid; i < V; i += SN) {
-        const float x = logit<DT>(row, i);
-        const uint32_t k = order_key(x);
-        if (k > key || (k == key && !ties)) above += w.of(x);
-      }
-      above = block_sum(above, s);
-      if (ties) above += ties * w.of(__uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key));
-      const double t = ceil(a.top_p * static_cast<double>(above));
-      uint64_t target = t < 1.0 ? 1 : static_cast<uint64_t>(t);
-      if (target > above) target = above;
-      find_prefix<DT, true>(row, V, w, target, s);
-      key = s.key;
-      ties = s.ties;
-      __syncthreads();
+      // tokens with less than (1 - top_p) / V of the maximum's weight are behind the last one kept
+      const double far = a.temperature * log(V / (1.0 - a.top_p)) * 1.0001;
+      find<DT, SW, true>(row, w, a.top_p, fminf(range, static_cast<float>(far)), xt, idt, s);
     }
-    if (ties) {   // the id of the last of the equal tokens that belong: runs of V / SN ids per thread
-      const int per = (V + SN - 1) / SN, i0 = tid * per, i1 = i0 + per < V ? i0 + per : V;
-      uint32_t c = 0;
-      for (int i = i0; i < i1; ++i) c += order_key(logit<DT>(row, i)) == key;
-      const uint64_t incl = wave_scan_u64(c, lane);
-      if (lane == 63) s.wave[wv] = incl;
-      if (tid == 0) s.id = V;
-      __syncthreads();
-      uint64_t at = incl - c;
-      for (int x = 0; x < wv; ++x) at += s.wave[x];
-      if (c && at < ties && at + c >= ties)
-        for (int i = i0; i < i1; ++i)
-          if (order_key(logit<DT>(row, i)) == key && ++at == ties) s.id = i;
-      __syncthreads();
-      last = s.id;
-      __syncthreads();
     }
-    auto kept = [&](int i) -> uint64_t {
-      if (i >= V) return 0;
-      const float x = logit<DT>(row, i);
-      const uint32_t k = order_key(x);
-      return k > key || (k == key && i <= last) ? w.kept(x) : 0;
-    };
-    // each wave a run of ids; then the wave, then the 64 ids, that the random number falls into
-    const int run = (V + SW * 64 - 1) / (SW * 64) * 64, i0 = wv * run;
+    // the wave, then the round, then the token that the random number falls into
     uint64_t mine = 0;
-#pragma unroll 2
-    for (int i = lane; i < run; i += 64) mine += kept(i0 + i);
+    if (!FILTER) {
+      row.each([&](float x, int id) { mine += Weigh::biased(w.real(x)); });
+      mine -= static_cast<uint64_t>(row.rounds) * 4 * Weigh::BIAS;
+    } else {
+      row.each4([&](const float (&x)[4], int id) {
+        bool in[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) in[e] = upto(x[e], id + e, xt, idt);
+        if (!__any(in[0] || in[1] || in[2] || in[3])) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint64_t v = w.kept(x[e]);
+          mine += in[e] ? v : 0;
+        }
+      });
+    }
     mine = wave_sum_u64(mine);
     if (lane == 0) s.wave[wv] = mine;
     __syncthreads();
-    uint64_t total = 0;
+    uint64_t total = 0, at = 0;
 #pragma unroll
-    for (int x = 0; x < SW; ++x) total += s.wave[x];
-    const int64_t ui = a.u_row ? a.u_row[*a.u_base + a.u_add + r] * a.u_ld + a.u_at : r;
-    const double f = static_cast<double>(a.u[ui]);
-    uint64_t target = total - 1;   // at least 1 kept: the maximum
-    if (f < 1.0) {
-      const double t = f * static_cast<double>(total);
-      target = t > 0.0 ? static_cast<uint64_t>(t) : 0;
-      if (target > total - 1) target = total - 1;
+    for (int x = 0; x < SW; ++x) {
+      if (x == wv) at = total;
+      total += s.wave[x];
     }
-    uint64_t at = 0;
-    for (int x = 0; x < wv; ++x) at += s.wave[x];
+    const uint64_t target = draw_target(u, total);   // at least the maximum is kept
     if (target >= at && target - at < mine) {   // this wave's
-      for (int i = 0; i < run; i += 64) {
-        const uint64_t incl = at + wave_scan_u64(kept(i0 + i + lane), lane);
-        const uint64_t hit = __ballot(incl > target);
-        if (hit) {
-          if (lane == 0) a.token[r] = i0 + i + static_cast<int>(__builtin_ctzll(hit));
+      for (int it = 0; it < row.rounds; ++it) {
+        float v[4];
+        row.load4(it, v);
+        uint64_t k[4], all = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int id = row.id0 + it * 256 + e;
+          k[e] = FILTER ? upto(v[e], id, xt, idt) ? w.kept(v[e]) : 0 : w.of(v[e]);
+          all += k[e];
+        }
+        const uint64_t incl = at + wave_scan_u64(all);
+        at = last_lane(incl);
+        if (at > target) {
+          const uint64_t hit = __ballot(incl > target);
+          if (lane == __builtin_ctzll(hit)) {
+            uint64_t c = incl - all;
+            int e = 0;
+            for (; e < 3; ++e) {
+              c += k[e];
+              if (c > target) break;
+            }
+            a.token[r] = row.id0 + it * 256 + e;
+          }
           break;
         }
-        at = (static_cast<uint64_t>(__shfl(static_cast<uint32_t>(incl >> 32), 63)) << 32) | __shfl(static_cast<uint32_t>(incl), 63);
       }
     }
-    __syncthreads();
   }
 }
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
   if (a.n_rows == 0) return hipSuccess;
   const dim3 grid(static_cast<unsigned>(a.n_rows < 65536 ? a.n_rows : 65536));
-  if (a.dtype == AIQ_F32)
-    hipLaunchKernelGGL((k_sample<AIQ_F32>), grid, dim3(SN), 0, s, a);
-  else if (a.dtype == AIQ_F16)
-    hipLaunchKernelGGL((k_sample<AIQ_F16>), grid, dim3(SN), 0, s, a);
-  else if (a.dtype == AIQ_BF16)
-    hipLaunchKernelGGL((k_sample<AIQ_BF16>), grid, dim3(SN), 0, s, a);
-  else
+  const bool filter = a.temperature > 0.0 && (a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0);
+  const bool wide = a.n_rows < 1024;
+#define AIQ_SAMPLE_K(DT_, SW_, F_) hipLaunchKernelGGL((k_sample<DT_, SW_, F_>), grid, dim3(64 * SW_), 0, s, a)
+#define AIQ_SAMPLE(DT_)                                        \
+  if (wide && filter) AIQ_SAMPLE_K(DT_, SW_MAX, true);         \
+  else if (wide) AIQ_SAMPLE_K(DT_, SW_MAX, false);             \
+  else if (filter) AIQ_SAMPLE_K(DT_, 4, true);                 \
+  else AIQ_SAMPLE_K(DT_, 4, false)
+  if (a.dtype == AIQ_F32) {
+    AIQ_SAMPLE(AIQ_F32);
+  } else if (a.dtype == AIQ_F16) {
+    AIQ_SAMPLE(AIQ_F16);
+  } else if (a.dtype == AIQ_BF16) {
+    AIQ_SAMPLE(AIQ_BF16);
+  } else {
     return hipErrorInvalidValue;
+  }
+#undef AIQ_SAMPLE
+#undef AIQ_SAMPLE_K
   return hipGetLastError();
 }
 
