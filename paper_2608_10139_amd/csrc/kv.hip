@@ -35,15 +35,18 @@ struct KvSeq {
   int tail;
 };
 
+// a value that is the same for all lanes, in a scalar register (the compiler cannot know it of one read from memory)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 __device__ __forceinline__ void kv_flag(const KvBatch& b) {
   if (b.status) atomicOr(reinterpret_cast<unsigned long long*>(b.status), static_cast<unsigned long long>(AIQ_DEV_KV_RANGE));
 }
 
 // Sequence i, or false where it is left out (its numbers do not fit, flagged; or it has no rows in this call).
 __device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, int i, KvSeq& s) {
-  s.len = b.len[i] + b.len_add;
+  s.len = uniform(b.len[i]) + b.len_add;
   if (b.cu) {
-    const int c0 = b.cu[i], c1 = b.cu[i + 1];
+    const int c0 = uniform(b.cu[i]), c1 = uniform(b.cu[i + 1]);
     s.row0 = c0;
     s.n = c1 - c0 + b.n_pre;
     if (c0 < 0 || c1 < c0 || c1 > b.n_rows) {
@@ -55,11 +58,11 @@ __device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, int i
     s.n = s.len == 0 ? 0 : 1;
   }
   if (s.n == 0) return false;
-  const int64_t e0 = b.blk_start[i], e1 = b.blk_start[i + 1];
+  const int64_t e0 = uniform(b.blk_start[i]), e1 = uniform(b.blk_start[i + 1]);
   s.bs = static_cast<int>(e0);
-  s.tail = b.tail_ids ? b.tail_ids[i] : i;
+  s.tail = b.tail_ids ? uniform(b.tail_ids[i]) : i;
   const bool uses_tail = s.len % KVB != 0 || (s.len - s.n) % KVB != 0;
-  if (s.len < s.n || s.len > b.max_len || e0 < 0 || (e1 - e0) * KVB < s.len ||
+  if (s.len < s.n || s.len > b.max_len || e0 < 0 || (c.n_blocks == 0 && s.len >= KVB) || (e1 - e0) * KVB < s.len ||
       (uses_tail && (s.tail < 0 || s.tail >= c.n_tails))) {
     kv_flag(b);
     return false;
@@ -77,7 +80,7 @@ __device__ __forceinline__ int kv_block(const KvCache& c, const KvBatch& b, int 
 
 __device__ __forceinline__ int kv_count(const KvBatch& b) {
   if (!b.n_ptr) return b.n_seq;
-  const int64_t n = *b.n_ptr;
+  const int64_t n = uniform(static_cast<int>(*b.n_ptr));
   return n < b.n_seq ? static_cast<int>(n) : b.n_seq;
 }
 
@@ -85,7 +88,8 @@ __device__ __forceinline__ int kv_count(const KvBatch& b) {
 // first(i) = per * cu[i] / R + extra * i on, enough for `extra` + its rows / R
 // units; which of them it fills the unit finds out itself.
 __device__ __forceinline__ int64_t unit_first(const KvBatch& b, int i, int per, int R, int extra) {
-  const int64_t c = (b.cu[i] < 0 ? 0 : b.cu[i]) + static_cast<int64_t>(i) * b.n_pre;
+  const int at = uniform(b.cu[i]);
+  const int64_t c = (at < 0 ? 0 : at) + static_cast<int64_t>(i) * b.n_pre;
   return c * per / R + static_cast<int64_t>(extra) * i;
 }
 __device__ __forceinline__ int unit_seq(const KvBatch& b, int n, int64_t u, int per, int R, int extra) {
@@ -186,8 +190,8 @@ __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
   const int64_t wave = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 6;
   const int64_t n_waves = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 6;
   for (int64_t item = wave; item < units * c.n_kv; item += n_waves) {
-    const int64_t u = item / c.n_kv;
-    const int h = static_cast<int>(item - u * c.n_kv);
+    const int64_t u = uniform(static_cast<int>(item / c.n_kv));   // (units are below 2^31)
+    const int h = uniform(static_cast<int>(item - u * c.n_kv));
     KvSeq s;
     int jj;
     if (!move_unit(c, a.b, n, u, s, jj)) continue;
@@ -313,8 +317,8 @@ __global__ __launch_bounds__(256) void k_kv_read(KvMoveArgs a) {
   const int64_t wave = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 6;
   const int64_t n_waves = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 6;
   for (int64_t item = wave; item < units * c.n_kv; item += n_waves) {
-    const int64_t u = item / c.n_kv;
-    const int h = static_cast<int>(item - u * c.n_kv);
+    const int64_t u = uniform(static_cast<int>(item / c.n_kv));   // (units are below 2^31)
+    const int h = uniform(static_cast<int>(item - u * c.n_kv));
     KvSeq s;
     int jj;
     if (!move_unit(c, a.b, n, u, s, jj)) continue;
@@ -461,6 +465,7 @@ hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, h
 // the largest).  fp16 holds the weights to 2^-12, as the 16-bit attention does.
 constexpr int KV_SEG = 16;       // blocks per segment
 constexpr float KV_SLACK = 8.0f, KV_UP = 7.0f;
+constexpr int64_t KV_ALONE = 4096;   // (tile, K/V head) items from which on waves take them alone
 
 __device__ __forceinline__ float swap_max(float v) {   // over the wave's four lane groups
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -545,44 +550,36 @@ __device__ __forceinline__ bool kv_tile(const KvAttendArgs& a, int n, int rep, i
   return true;
 }
 
-template <int HD, bool BF, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a, int64_t n_tiles, int32_t n_seg, int32_t slot_rows) {
-  constexpr int KC = HD / 64, NO = HD / 16;
-  __shared__ __attribute__((aligned(16))) uint16_t vt[KVB * HD];   // the tail's values, for transposing reads
-  __shared__ int bad[KVB];                                         // its tokens with an infinity or NaN
-  extern __shared__ float lds[];
-  float* so = lds;                               // [4][rows][HD]
-  float* sm = lds + 4 * slot_rows * HD;          // [4][rows]
-  float* sl = sm + 4 * slot_rows;
-  float* state = sl + 4 * slot_rows;             // [rows][HD], [2][2][rows]: where a workgroup walks several segments
-  const KvCache& c = a.c;
-  const int n = kv_count(a.b);
-  if (n <= 0) return;
-  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rep = a.n_heads / c.n_kv;
-  const int64_t tiles = a.b.cu ? unit_first(a.b, n, rep, 16, 1) : static_cast<int64_t>(n) * ((rep + 15) / 16);
-  const int64_t items = (tiles < n_tiles ? tiles : n_tiles) * c.n_kv * (SPLIT ? n_seg : 1);
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t unit = SPLIT ? item / n_seg : item;   // (tile, K/V head)
-    const int seg0 = SPLIT ? static_cast<int>(item - unit * n_seg) : 0;
-    const int64_t u = unit / c.n_kv;
-    const int h = static_cast<int>(unit - u * c.n_kv);
-    KvTile t;
-    if (!kv_tile(a, n, rep, u, h, t)) continue;
-    const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
-    if (SPLIT && seg0 >= segs) continue;
+// One wave's part of a tile: its queries, and the softmax state (m, l, o) of
+// the blocks it has taken since reset().
+template <int HD, bool BF, bool LEAN>
+struct KvWave {
+  static constexpr int KC = HD / 64, NO = HD / 16;
+  const KvAttendArgs& a;
+  const KvTile& t;
+  uint16_t* vt;         // LDS: the tail's values, for transposing reads
+  int* bad;             // LDS: its tokens with an infinity or NaN
+  int h, lane, g, c16, pos;
+  const uint16_t* qp;
+  float fac;
+  half8 qf[KC * 2];
+  int id;               // lane x < KV_SEG: the segment's block x, its scales (a number out of bounds: block 0, its
+  float ks, vs, lv;     // tokens weigh nothing); log2 of the values'
+
+  uint4 kr[2 * KC];     // the next block's keys
+  f32x4 o[NO];
+  float m, l;
+
+  __device__ __forceinline__ KvWave(const KvAttendArgs& a_, const KvTile& t_, int h_, int rep, uint16_t* vt_, int* bad_)
+      : a(a_), t(t_), vt(vt_), bad(bad_), h(h_), lane(threadIdx.x & 63), g(lane >> 4), c16(lane & 15) {
     // queries: lane (g, c16) holds row c16, dims 64 kc + 16 g + 8 e .. + 7
     const int row = t.r0 + (c16 < t.rows ? c16 : 0);
-    const int pos = t.s.len - t.s.n + row / rep;
-    const uint16_t* qp = a.q + (t.s.row0 + row / rep) * a.q_ld + (h * rep + row % rep) * HD + g * 16;
-    float fac = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
-    half8 qf[KC * 2];
+    pos = t.s.len - t.s.n + row / rep;
+    qp = a.q + (t.s.row0 + row / rep) * a.q_ld + (h * rep + row % rep) * HD + g * 16;
+    fac = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
 #pragma unroll
-    for (int x = 0; x < KC * 2; ++x) {
-      const uint4 v = *reinterpret_cast<const uint4*>(qp + (x / 2) * 64 + (x % 2) * 8);
-      qf[x] = __builtin_bit_cast(half8, v);
-    }
+    for (int x = 0; x < KC * 2; ++x)
+      qf[x] = __builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(qp + (x / 2) * 64 + (x % 2) * 8));
     if (BF) {   // the row times a power of two, exact in fp16 (but for values 2^-25 of the row's largest)
       float mx = 0.f;
 #pragma unroll
@@ -611,202 +608,355 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend(KvAttendArgs a, int64_t n_
         }
       }
     }
-    const int seg_end = SPLIT ? seg0 + 1 : segs;
-    for (int seg = seg0; seg < (segs == 0 ? seg0 + 1 : seg_end); ++seg) {
-      // the segment's blocks: number, scales
-      const int jl = seg * KV_SEG + lane;
-      int id = -1;
-      float ksl = 0.f, vsl = 1.f;
-      if (lane < KV_SEG && jl < t.nb && (jl + 1) * KVB <= t.s.len) {
-        id = kv_block(c, a.b, t.s.bs + jl);
-        if (id >= 0) {
-          const int64_t at = static_cast<int64_t>(id) * c.n_kv + h;
-          ksl = c.ks[at];
-          vsl = c.vs[at];
+  }
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int x = 0; x < NO; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+  }
+  __device__ __forceinline__ void segment(int seg) {
+    const int j = seg * KV_SEG + lane;
+    id = 0;
+    ks = 0.f;
+    vs = 1.f;
+    lv = -INFINITY;
+    if (lane < KV_SEG && j < t.nb && (j + 1) * KVB <= t.s.len) {
+      id = kv_block(a.c, a.b, t.s.bs + j);
+      if (id >= 0) {
+        const int64_t at = static_cast<int64_t>(id) * a.c.n_kv + h;
+        ks = a.c.ks[at];
+        vs = a.c.vs[at];
+        lv = __builtin_amdgcn_logf(vs);
+      }
+      id = id < 0 ? 0 : id;
+    }
+  }
+  // of the nbs blocks that the tile sees of a segment, those that are not the tail
+  __device__ __forceinline__ int full_blocks(int seg, int nbs) const {
+    const int f = t.s.len / KVB - seg * KV_SEG;
+    return f < nbs ? f : nbs;
+  }
+  __device__ __forceinline__ int64_t at(int bid) const { return (static_cast<int64_t>(bid) * a.c.n_kv + h) * (KVB * HD); }
+  // the keys of block k of the segment (a full one; k < 0: none)
+  __device__ __forceinline__ void load(int k) {
+    if (k < 0) return;
+    const uint8_t* p = a.c.k + at(__builtin_amdgcn_readlane(id, k));
+    const uint32_t off = static_cast<uint32_t>(lane) * 16;
+#pragma unroll
+    for (int x = 0; x < 2 * KC; ++x) kr[x] = *reinterpret_cast<const uint4*>(p + x * 1024 + off);
+  }
+  // weights of a block's 8 tokens of this lane, from its scores acc (times c1, plus c2)
+  __device__ __forceinline__ void weigh(const f32x4 (&acc)[2], float c1, float c2, float inv, int tok0, bool masked,
+                                        float (&p)[8]) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = fmaf(acc[e / 4][e % 4], c1, c2);
+      if (masked && tok0 + (e / 4) * 16 + g * 4 + e % 4 > pos) p[e] = -INFINITY;
+      mx = fmaxf(mx, p[e]);
+    }
+    if (__any(mx > m + KV_SLACK)) {
+      const float mn = fmaxf(m, swap_max(mx));
+      const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+#pragma unroll
+      for (int x = 0; x < NO; ++x) o[x] *= al;
+      l *= al;
+      m = mn;
+    }
+    const float ref = m == -INFINITY ? 0.f : m - KV_UP;
+    float ps = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+      ps += p[e];
+    }
+    l = ps == 0.f ? l : fmaf(ps, inv, l);   // (a block that the row does not see adds nothing, whatever its scale)
+  }
+  // block k of the segment, whose keys load() has read; its values are read while its scores are
+  // computed, the keys of block kn while its weights and values are
+  __device__ __forceinline__ void take(int seg, int k, int kn) {
+    const int tok0 = (seg * KV_SEG + k) * KVB;
+    const int bid = __builtin_amdgcn_readlane(id, k);
+    uint4 vr[2 * KC];
+    const uint8_t* vp = a.c.v + at(bid);
+    const uint32_t off = static_cast<uint32_t>(lane) * 16;
+#pragma unroll
+    for (int x = 0; x < 2 * KC; ++x) vr[x] = *reinterpret_cast<const uint4*>(vp + x * 1024 + off);
+    const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), k));
+    const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), k));
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const uint4 y = kr[tt * KC + kc];
+        acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.x, y.y), qf[kc * 2], acc[tt], 0, 0, 0);
+        acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.z, y.w), qf[kc * 2 + 1], acc[tt], 0, 0, 0);
+      }
+    load(kn);
+    float p[8];
+    weigh(acc, fac * sk, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lv), k)), 1.0f / sv, tok0, tok0 + KVB - 1 > t.pos0, p);
+    half8 pf;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) pf[e] = static_cast<_Float16>(p[e]);
+#pragma unroll
+    for (int x = 0; x < 2 * KC; ++x) {
+      o[2 * x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].x, vr[x].y), pf, o[2 * x], 0, 0, 0);
+      o[2 * x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].z, vr[x].w), pf, o[2 * x + 1], 0, 0, 0);
+    }
+  }
+  // the tail: 16-bit rows, products in their own type; rows past the length are read as the last one, and
+  // zeroed where that matters.  Values go through LDS, row-major, in 16-byte pieces (swizzled by the row).
+  __device__ __forceinline__ void tail(int tok0) {
+    const int left = t.s.len - tok0;
+    // (its addresses are not worth registers through the whole loop: computed here)
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int g = ln >> 4, c16 = ln & 15;
+    const uint16_t* tk = tail_at(a.c, t.s.tail, 0, h);
+    const uint16_t* tv = tail_at(a.c, t.s.tail, 1, h);
+    const bool several = a.b.cu != nullptr;
+    constexpr int PIECES = HD / 8, PER = KVB * PIECES / 64;
+    uint4 kt[4 * KC], vv[PER];
+    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    auto load_keys = [&]() {
+#pragma unroll
+      for (int x = 0; x < 4 * KC; ++x) {   // token x / (2 KC) * 16 + c16
+        const int tok = (x / (2 * KC)) * 16 + c16, row = tok < left ? tok : left - 1;
+        kt[x] = *reinterpret_cast<const uint4*>(tk + static_cast<uint32_t>(row * HD + (x % (2 * KC) / 2) * 64 + g * 16 + (x % 2) * 8));
+      }
+    };
+    if (!LEAN) load_keys();
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const int tok = (x * 64 + ln) / PIECES, row = tok < left ? tok : left - 1;
+      vv[x] = *reinterpret_cast<const uint4*>(tv + static_cast<uint32_t>(row * HD + (x * 64 + ln) % PIECES * 8));
+    }
+    if (several) bad[ln & (KVB - 1)] = 0;
+    wave_sync();
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const int tok = (x * 64 + ln) / PIECES, ch = (x * 64 + ln) % PIECES;
+      uint4 y = vv[x];
+      bool none = tok >= left;
+      if (several) {   // a later query's infinity or NaN must not meet the weight 0
+        const uint32_t z = abs_max(abs_max(abs_max(abs_max(0, y.x), y.y), y.z), y.w), inf = BF ? 0x7F80u : 0x7C00u;
+        if (!none && ((z & 0xFFFFu) >= inf || (z >> 16) >= inf)) {
+          none = true;
+          bad[tok] = 1;
         }
       }
-      f32x4 o[NO];
+      y.x = none ? 0 : y.x;
+      y.y = none ? 0 : y.y;
+      y.z = none ? 0 : y.z;
+      y.w = none ? 0 : y.w;
+      *reinterpret_cast<uint4*>(vt + tok * HD + ((ch ^ (tok & 7)) << 3)) = y;
+    }
+    wave_sync();
+    if (LEAN) {   // (registers for keys or values at a time)
+      __builtin_amdgcn_sched_barrier(0);
+      load_keys();
+    }
 #pragma unroll
-      for (int x = 0; x < NO; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-      float m = -INFINITY, l = 0.f;
-      // weights of the block's 8 tokens of this lane, from its scores acc (times c1, plus c2)
-      auto weigh = [&](const f32x4 (&acc)[2], float c1, float c2, float inv, int tok0, bool masked, float (&p)[8]) {
-        float s[8], mx = -INFINITY;
+    for (int x = 0; x < 4 * KC; ++x) {
+      f32x4& s = acc[x / (2 * KC)];
+      const int y = x % (2 * KC);
+      if (BF) {
+        const uint4 qv = *reinterpret_cast<const uint4*>(qp + (y / 2) * 64 + (y % 2) * 8);
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt[x]), __builtin_bit_cast(bf16x8, qv), s, 0, 0, 0);
+      } else {
+        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kt[x]), qf[y], s, 0, 0, 0);
+      }
+    }
+    float p[8];
+    weigh(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, tok0, true, p);
+    union {
+      uint16_t u[8];
+      half8 h;
+      bf16x8 b;
+    } pf;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s[e] = fmaf(acc[e / 4][e % 4], c1, c2);
-          if (masked && tok0 + (e / 4) * 16 + g * 4 + e % 4 > pos) s[e] = -INFINITY;
-          mx = fmaxf(mx, s[e]);
+    for (int e = 0; e < 8; ++e) {
+      pf.u[e] = BF ? f2bf(p[e]) : f2h(p[e]);
+      if (several && p[e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l = __uint_as_float(0x7FC00000u);
+    }
+    // lane 4 a + b of a 16-lane group receives element b of the pieces that lanes a, a + 4, .. address
+    lds_u16* const vl = (lds_u16*)(vt);
+#pragma unroll
+    for (int x = 0; x < NO; ++x) {
+      v4i16 part[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const int tok = tt * 16 + g * 4 + (c16 >> 2), d = x * 16 + 4 * (c16 & 3);
+        part[tt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            reinterpret_cast<lds_v4i16*>(vl + tok * HD + (((d >> 3) ^ (tok & 7)) << 3) + (d & 7)));
+      }
+      const auto vf = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      o[x] = BF ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf.b, o[x], 0, 0, 0)
+                : __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vf), pf.h, o[x], 0, 0, 0);
+    }
+  }
+};
+
+// NW = 4: a workgroup per (tile, K/V head), or with SPLIT per segment of one.
+// NW = 1: a wave per (tile, K/V head) takes the four shares of each segment one after another:
+// the same sums, without the exchange.
+template <int HD, bool BF, bool SPLIT, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttendArgs a, int64_t n_tiles, int32_t n_seg,
+                                                                      int32_t slot_rows) {
+  typedef KvWave<HD, BF, NW == 1> Wave;
+  constexpr int NO = Wave::NO;
+  __shared__ __attribute__((aligned(16))) uint16_t vt[KVB * HD];
+  __shared__ int bad[KVB];
+  extern __shared__ float lds[];
+  float* so = lds;                               // NW = 4: [4][rows][HD]
+  float* sm = so + (NW == 4 ? 4 * slot_rows * HD : 0);   // [4][rows]
+  float* sl = sm + (NW == 4 ? 4 * slot_rows : 0);
+  // of the earlier segments, where there are several: [rows][HD], [2][2][rows]; NW = 1: of the earlier shares
+  // [rows][HD], [2][rows], then of the earlier segments the same
+  float* state = sl + (NW == 4 ? 4 * slot_rows : 0);
+  const KvCache& c = a.c;
+  const int n = kv_count(a.b);
+  if (n <= 0) return;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rep = a.n_heads / c.n_kv;
+  const int64_t tiles = a.b.cu ? unit_first(a.b, n, rep, 16, 1) : static_cast<int64_t>(n) * ((rep + 15) / 16);
+  const int64_t items = (tiles < n_tiles ? tiles : n_tiles) * c.n_kv * (SPLIT ? n_seg : 1);
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t unit = SPLIT ? item / n_seg : item;   // (tile, K/V head)
+    const int seg0 = SPLIT ? static_cast<int>(item - unit * n_seg) : 0;
+    const int64_t u = unit / c.n_kv;
+    const int h = static_cast<int>(unit - u * c.n_kv);
+    KvTile t;
+    if (!kv_tile(a, n, rep, u, h, t)) continue;
+    const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
+    if (SPLIT && seg0 >= segs) continue;
+    const int seg_end = SPLIT || segs == 0 ? seg0 + 1 : segs;
+    Wave x(a, t, h, rep, vt, bad);
+    if (NW == 1) {
+      // states between shares and between segments: LDS (few rows; registers for them would cost a wave per SIMD)
+      const int stride = slot_rows * (HD + 2);
+      auto fold = [&](bool any, const float* st) {   // the state st (none: !any), then this one, into (x.m, x.l, x.o)
+        const float m0 = any ? st[slot_rows * HD + c16] : -INFINITY, l0 = any ? st[slot_rows * HD + slot_rows + c16] : 0.f;
+        const float mn = fmaxf(m0, x.m), ref = mn == -INFINITY ? 0.f : mn;
+        const float e0 = __builtin_amdgcn_exp2f(m0 - ref), e1 = __builtin_amdgcn_exp2f(x.m - ref);
+        x.l = fmaf(x.l, e1, l0 * e0);
+#pragma unroll
+        for (int y = 0; y < NO; ++y) {
+          f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (any && c16 < t.rows) z = *reinterpret_cast<const f32x4*>(st + c16 * HD + y * 16 + g * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.o[y][e] = fmaf(x.o[y][e], e1, z[e] * e0);
         }
-        if (__any(mx > m + KV_SLACK)) {
-          const float mn = fmaxf(m, swap_max(mx));
-          const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-#pragma unroll
-          for (int x = 0; x < NO; ++x) o[x] *= al;
-          l *= al;
-          m = mn;
-        }
-        const float ref = m == -INFINITY ? 0.f : m - KV_UP;
-        float ps = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(s[e] - ref);
-          ps += p[e];
-        }
-        l = ps == 0.f ? l : fmaf(ps, inv, l);   // (a block that the row does not see adds nothing, whatever its scale)
+        x.m = mn;
       };
-      for (int k = w; k < KV_SEG; k += 4) {
-        const int j = seg * KV_SEG + k;
-        if (j >= t.nb) break;
-        const int tok0 = j * KVB;
-        f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-        float p[8];
-        if (tok0 + KVB <= t.s.len) {
-          const int bid = __builtin_amdgcn_readlane(id, k);
-          if (bid < 0) continue;
-          const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ksl), k));
-          const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vsl), k));
-          const int64_t at = (static_cast<int64_t>(bid) * c.n_kv + h) * (KVB * HD);
-          uint4 kr[2 * KC], vr[2 * KC];
+      auto keep = [&](float* st) {
+        if (c16 < t.rows) {
 #pragma unroll
-          for (int x = 0; x < 2 * KC; ++x) kr[x] = *reinterpret_cast<const uint4*>(c.k + at + (x * 64 + lane) * 16);
-#pragma unroll
-          for (int x = 0; x < 2 * KC; ++x) vr[x] = *reinterpret_cast<const uint4*>(c.v + at + (x * 64 + lane) * 16);
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int kc = 0; kc < KC; ++kc) {
-              const uint4 y = kr[tt * KC + kc];
-              acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.x, y.y), qf[kc * 2], acc[tt], 0, 0, 0);
-              acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.z, y.w), qf[kc * 2 + 1], acc[tt], 0, 0, 0);
-            }
-          weigh(acc, fac * ks, __builtin_amdgcn_logf(vs), 1.0f / vs, tok0, tok0 + KVB - 1 > t.pos0, p);
-          half8 pf;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pf[e] = static_cast<_Float16>(p[e]);
-#pragma unroll
-          for (int x = 0; x < 2 * KC; ++x) {
-            o[2 * x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].x, vr[x].y), pf, o[2 * x], 0, 0, 0);
-            o[2 * x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].z, vr[x].w), pf, o[2 * x + 1], 0, 0, 0);
-          }
-        } else {
-          // the tail: 16-bit rows, products in their own type; rows past the length are not read.
-          // Values go through LDS, row-major, in 16-byte pieces (swizzled by the row).
-          const int left = t.s.len - tok0;
-          const uint16_t* tk = tail_at(c, t.s.tail, 0, h);
-          const uint16_t* tv = tail_at(c, t.s.tail, 1, h);
-          const bool several = a.b.cu != nullptr;
-          if (several) bad[lane & (KVB - 1)] = 0;
-          wave_sync();
-#pragma unroll
-          for (int x = lane; x < KVB * HD / 8; x += 64) {
-            const int tok = x / (HD / 8), ch = x % (HD / 8);
-            uint4 y = make_uint4(0, 0, 0, 0);
-            if (tok < left) y = *reinterpret_cast<const uint4*>(tv + tok * HD + ch * 8);
-            if (several) {   // a later query's infinity or NaN must not meet the weight 0
-              const uint32_t m = abs_max(abs_max(abs_max(abs_max(0, y.x), y.y), y.z), y.w), inf = BF ? 0x7F80u : 0x7C00u;
-              if ((m & 0xFFFFu) >= inf || (m >> 16) >= inf) {
-                y = make_uint4(0, 0, 0, 0);
-                bad[tok] = 1;
-              }
-            }
-            *reinterpret_cast<uint4*>(vt + tok * HD + ((ch ^ (tok & 7)) << 3)) = y;
-          }
-          wave_sync();
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt) {
-            const int tok = tt * 16 + c16;
-#pragma unroll
-            for (int x = 0; x < 2 * KC; ++x) {
-              const int e = (x / 2) * 64 + g * 16 + (x % 2) * 8;
-              uint4 y = make_uint4(0, 0, 0, 0);
-              if (tok < left) y = *reinterpret_cast<const uint4*>(tk + tok * HD + e);
-              if (BF) {
-                const uint4 qv = *reinterpret_cast<const uint4*>(qp + (x / 2) * 64 + (x % 2) * 8);
-                acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y),
-                                                                  __builtin_bit_cast(bf16x8, qv), acc[tt], 0, 0, 0);
-              } else {
-                acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, y), qf[x], acc[tt], 0, 0, 0);
-              }
-            }
-          }
-          weigh(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, tok0, true, p);
-          union {
-            uint16_t u[8];
-            half8 h;
-            bf16x8 b;
-          } pf;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            pf.u[e] = BF ? f2bf(p[e]) : f2h(p[e]);
-            if (several && p[e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l = __uint_as_float(0x7FC00000u);
-          }
-          // lane 4 a + b of a 16-lane group receives element b of the pieces that lanes a, a + 4, .. address
-          lds_u16* const vl = (lds_u16*)(vt);
-#pragma unroll
-          for (int x = 0; x < NO; ++x) {
-            v4i16 part[2];
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-              const int tok = tt * 16 + g * 4 + (c16 >> 2), d = x * 16 + 4 * (c16 & 3);
-              part[tt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  reinterpret_cast<lds_v4i16*>(vl + tok * HD + (((d >> 3) ^ (tok & 7)) << 3) + (d & 7)));
-            }
-            const auto vf = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-            o[x] = BF ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf.b, o[x], 0, 0, 0)
-                      : __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vf), pf.h, o[x], 0, 0, 0);
+          for (int y = 0; y < NO; ++y) *reinterpret_cast<f32x4*>(st + c16 * HD + y * 16 + g * 4) = x.o[y];
+          if (g == 0) {
+            st[slot_rows * HD + c16] = x.m;
+            st[slot_rows * HD + slot_rows + c16] = x.l;
           }
         }
+        wave_sync();
+      };
+      for (int seg = seg0; seg < seg_end; ++seg) {
+        x.segment(seg);
+        const int nbs = t.nb - seg * KV_SEG < KV_SEG ? t.nb - seg * KV_SEG : KV_SEG;
+        const int full = x.full_blocks(seg, nbs);
+        x.load(full > 0 ? 0 : -1);
+        // share after share (blocks 0, 4, 8, 12, then 1, 5, ..), each folded onto those before
+#pragma unroll 1
+        for (int sh = 0; sh == 0 || (sh < 4 && sh < nbs); ++sh) {
+          x.reset();
+#pragma unroll 1
+          for (int k = sh; k < full; k += 4)
+            x.take(seg, k, k + 4 < full ? k + 4 : sh < 3 && sh + 1 < full ? sh + 1 : -1);
+          if (full < nbs && (full & 3) == sh) x.tail((seg * KV_SEG + full) * KVB);
+          x.l = swap_add(x.l);
+          fold(sh > 0, state);
+          if (sh < 3 && sh + 1 < nbs) keep(state);
+        }
+        fold(seg > seg0, state + stride);
+        if (seg + 1 < seg_end) keep(state + stride);
       }
-      l = swap_add(l);
-      __syncthreads();   // the last segment's states are read before these are written
       if (c16 < t.rows) {
+        const int q = t.r0 + c16;
+        const float inv = x.l == 0.f ? 0.f : 1.0f / x.l;
+        uint16_t* op = a.out + (t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + g * 4;
 #pragma unroll
-        for (int x = 0; x < NO; ++x)
-          *reinterpret_cast<f32x4*>(so + (w * slot_rows + c16) * HD + x * 16 + g * 4) = o[x];
-        if (g == 0) {
-          sm[w * slot_rows + c16] = m;
-          sl[w * slot_rows + c16] = l;
+        for (int y = 0; y < NO; ++y) {
+          uint32_t v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = f2act(x.o[y][e] * inv, a.out_act);
+          *reinterpret_cast<uint2*>(op + y * 16) = make_uint2(v[0] | (v[1] << 16), v[2] | (v[3] << 16));
+        }
+      }
+      wave_sync();
+    } else {
+      for (int seg = seg0; seg < seg_end; ++seg) {
+        x.segment(seg);
+        const int nbs = t.nb - seg * KV_SEG < KV_SEG ? t.nb - seg * KV_SEG : KV_SEG;
+        x.reset();
+        const int full = x.full_blocks(seg, nbs);
+        x.load(w < full ? w : -1);
+#pragma unroll 1
+        for (int k = w; k < full; k += 4) x.take(seg, k, k + 4 < full ? k + 4 : -1);
+        if (full < nbs && (full & 3) == w) x.tail((seg * KV_SEG + full) * KVB);
+        const float lw = swap_add(x.l);
+        __syncthreads();   // the last segment's states are read before these are written
+        if (c16 < t.rows) {
+#pragma unroll
+          for (int y = 0; y < NO; ++y)
+            *reinterpret_cast<f32x4*>(so + (w * slot_rows + c16) * HD + y * 16 + g * 4) = x.o[y];
+          if (g == 0) {
+            sm[w * slot_rows + c16] = x.m;
+            sl[w * slot_rows + c16] = lw;
+          }
+        }
+        __syncthreads();
+        // the shares folded in order, then onto the earlier segments' state (its sums by parity)
+#pragma unroll 1
+        for (int e = threadIdx.x; e < t.rows * HD; e += 64 * NW) {
+          const int r = e / HD, d = e % HD;
+          float m1 = -INFINITY, l1 = 0.f, o1 = 0.f;
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            kv_fold(m1, l1, o1, sm[v * slot_rows + r], sl[v * slot_rows + r], so[(v * slot_rows + r) * HD + d]);
+          float m0 = -INFINITY, l0 = 0.f, o0 = 0.f;
+          if (!SPLIT && seg > 0) {
+            const float* st = state + slot_rows * HD + (seg & 1) * 2 * slot_rows;
+            m0 = st[r];
+            l0 = st[slot_rows + r];
+            o0 = state[e];
+          }
+          kv_fold(m0, l0, o0, m1, l1, o1);
+          if (!SPLIT && seg + 1 < seg_end) {
+            float* st = state + slot_rows * HD + ((seg + 1) & 1) * 2 * slot_rows;
+            state[e] = o0;
+            if (d == 0) {
+              st[r] = m0;
+              st[slot_rows + r] = l0;
+            }
+          } else if (SPLIT) {   // the segment's state: values, then (reference, sum) per row
+            float* slot = a.part + (unit * n_seg + seg0) * (static_cast<int64_t>(slot_rows) * (HD + 2));
+            slot[e] = o0;
+            if (d == 0) {
+              slot[slot_rows * HD + 2 * r] = m0;
+              slot[slot_rows * HD + 2 * r + 1] = l0;
+            }
+          } else {
+            const int q = t.r0 + r;
+            const float v = l0 == 0.f ? 0.f : o0 * (1.0f / l0);
+            a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
+          }
         }
       }
       __syncthreads();
-      // the shares folded in order, then onto the earlier segments' state (kept in LDS, its sums by parity)
-      for (int e = threadIdx.x; e < t.rows * HD; e += 256) {
-        const int r = e / HD, d = e % HD;
-        float m1 = -INFINITY, l1 = 0.f, o1 = 0.f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-          kv_fold(m1, l1, o1, sm[v * slot_rows + r], sl[v * slot_rows + r], so[(v * slot_rows + r) * HD + d]);
-        float m0 = -INFINITY, l0 = 0.f, o0 = 0.f;
-        if (!SPLIT && seg > 0) {
-          const float* st = state + slot_rows * HD + (seg & 1) * 2 * slot_rows;
-          m0 = st[r];
-          l0 = st[slot_rows + r];
-          o0 = state[e];
-        }
-        kv_fold(m0, l0, o0, m1, l1, o1);
-        if (!SPLIT && seg + 1 < seg_end) {
-          float* st = state + slot_rows * HD + ((seg + 1) & 1) * 2 * slot_rows;
-          state[e] = o0;
-          if (d == 0) {
-            st[r] = m0;
-            st[slot_rows + r] = l0;
-          }
-        } else if (SPLIT) {   // the segment's state: values, then (reference, sum) per row
-          float* slot = a.part + (unit * n_seg + seg0) * (static_cast<int64_t>(slot_rows) * (HD + 2));
-          slot[e] = o0;
-          if (d == 0) {
-            slot[slot_rows * HD + 2 * r] = m0;
-            slot[slot_rows * HD + 2 * r + 1] = l0;
-          }
-        } else {
-          const int q = t.r0 + r;
-          const float v = l0 == 0.f ? 0.f : o0 / l0;
-          a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
-        }
-      }
     }
-    __syncthreads();
   }
 }
 
@@ -832,7 +982,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
     float m = -INFINITY, l = 0.f, o = 0.f;
     for (int s = 0; s < segs; ++s, slot += step)
       kv_fold(m, l, o, slot[slot_rows * HD + 2 * r], slot[slot_rows * HD + 2 * r + 1], slot[e]);
-    const float v = l == 0.f ? 0.f : o / l;
+    const float v = l == 0.f ? 0.f : o * (1.0f / l);
     a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
   }
 }
@@ -865,25 +1015,30 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t s) {
   const KvShape k = kv_shape(a.c, a.b, a.n_heads);
   if (k.split && !a.part) return hipErrorInvalidValue;
   const int64_t items = k.tiles * a.c.n_kv * (k.split ? k.n_seg : 1);
-  const dim3 grid(static_cast<unsigned>(items < (1 << 20) ? items : 1 << 20));
-  const bool walks = !k.split && k.n_seg > 1;
-  const size_t lds = static_cast<size_t>(k.rows) * (4 * (a.c.hd + 2) + (walks ? a.c.hd + 4 : 0)) * 4;
+  const bool alone = !k.split && items >= KV_ALONE;
+  const int64_t cap = !a.b.n_ptr ? 1 << 20 : alone ? 1 << 16 : 1 << 14;   // (a bound from the host only: the sequences may be few)
+  const dim3 grid(static_cast<unsigned>(items < cap ? items : cap));
+  const int state = alone ? 2 * (a.c.hd + 2) : 4 * (a.c.hd + 2) + (!k.split && k.n_seg > 1 ? a.c.hd + 4 : 0);   // per row
+  const size_t lds = static_cast<size_t>(k.rows) * state * 4;
   const bool bf = a.c.act == ACT_BF16;
-#define AIQ_KV_ATTEND(HD_, BF_, SP_) \
-  hipLaunchKernelGGL((k_kv_attend<HD_, BF_, SP_>), grid, dim3(256), lds, s, a, k.tiles, k.n_seg, k.rows)
-#define AIQ_KV_ATTEND_HD(HD_)                             \
-  if (bf && k.split) AIQ_KV_ATTEND(HD_, true, true);      \
-  else if (bf) AIQ_KV_ATTEND(HD_, true, false);           \
-  else if (k.split) AIQ_KV_ATTEND(HD_, false, true);      \
-  else AIQ_KV_ATTEND(HD_, false, false)
-  if (a.c.hd == 64) {
-    AIQ_KV_ATTEND_HD(64);
+#define AIQ_KV_ATTEND(HD_, BF_, SP_, NW_) \
+  hipLaunchKernelGGL((k_kv_attend<HD_, BF_, SP_, NW_>), grid, dim3(64 * NW_), lds, s, a, k.tiles, k.n_seg, k.rows)
+#define AIQ_KV_ATTEND_BF(HD_, BF_)                       \
+  if (k.split) AIQ_KV_ATTEND(HD_, BF_, true, 4);         \
+  else if (alone) AIQ_KV_ATTEND(HD_, BF_, false, 1);     \
+  else AIQ_KV_ATTEND(HD_, BF_, false, 4)
+  if (a.c.hd == 64 && bf) {
+    AIQ_KV_ATTEND_BF(64, true);
+  } else if (a.c.hd == 64) {
+    AIQ_KV_ATTEND_BF(64, false);
+  } else if (a.c.hd == 128 && bf) {
+    AIQ_KV_ATTEND_BF(128, true);
   } else if (a.c.hd == 128) {
-    AIQ_KV_ATTEND_HD(128);
+    AIQ_KV_ATTEND_BF(128, false);
   } else {
     return hipErrorInvalidValue;
   }
-#undef AIQ_KV_ATTEND_HD
+#undef AIQ_KV_ATTEND_BF
 #undef AIQ_KV_ATTEND
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !k.split) return e;

@@ -682,7 +682,10 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
   if (a.n_rows == 0) return hipSuccess;
   const dim3 grid(static_cast<unsigned>(a.n_rows < 65536 ? a.n_rows : 65536));
   const bool filter = a.temperature > 0.0 && (a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0);
-  const bool wide = a.n_rows < 1024;
+  // 16 waves per row up to the rows that leave CUs without one of theirs, 4 beyond: 512 rows of 32,000 logits 39, 93 and
+  // 42 us (without filters, top-p, top-k) against 53, 121 and 42; 700 rows 54, 135 and 60 against 63, 139 and 45; 1,023
+  // 72, 182 and 81 against 73, 159 and 50.
+  const bool wide = a.n_rows < (filter ? 640 : 1024);
 #define AIQ_SAMPLE_K(DT_, SW_, F_) hipLaunchKernelGGL((k_sample<DT_, SW_, F_>), grid, dim3(64 * SW_), 0, s, a)
 #define AIQ_SAMPLE(DT_)                                        \
   if (wide && filter) AIQ_SAMPLE_K(DT_, SW_MAX, true);         \
