@@ -465,6 +465,7 @@ hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, h
 // the largest).  fp16 holds the weights to 2^-12, as the 16-bit attention does.
 constexpr int KV_SEG = 16;       // blocks per segment
 constexpr float KV_SLACK = 8.0f, KV_UP = 7.0f;
+constexpr int KV_MANY = 48;          // rows per sequence from which on tiles of KV_ROWS take them
 constexpr int64_t KV_ALONE = 4096;   // (tile, K/V head) items from which on waves take them alone
 
 __device__ __forceinline__ float swap_max(float v) {   // over the wave's four lane groups
@@ -501,6 +502,70 @@ __device__ __forceinline__ half8 bytes_f16(uint32_t lo, uint32_t hi) {
   return x.h - off;
 }
 
+// bf16 query fragments (a row's in the lanes of one column) as fp16 times a power of two, exact but for values
+// 2^-25 of the row's largest; returns the power that undoes it
+template <int N>
+__device__ __forceinline__ float rows_f16(half8 (&q)[N]) {
+  float mx = 0.f;
+#pragma unroll
+  for (int x = 0; x < N; ++x) {
+    const uint4 v = __builtin_bit_cast(uint4, q[x]);
+    const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      mx = fmaxf(mx, fabsf(__uint_as_float(y[e] << 16)));
+      mx = fmaxf(mx, fabsf(__uint_as_float(y[e] & 0xFFFF0000u)));
+    }
+  }
+  mx = swap_max(mx);
+  int ex = static_cast<int>(__float_as_uint(mx) >> 23) - 127;   // mx in [2^ex, 2^(ex + 1))
+  ex = ex < -100 ? -100 : ex;
+  const float up = __uint_as_float(static_cast<uint32_t>(127 + 8 - ex) << 23);
+#pragma unroll
+  for (int x = 0; x < N; ++x) {
+    const uint4 v = __builtin_bit_cast(uint4, q[x]);
+    const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      q[x][2 * e] = static_cast<_Float16>(__uint_as_float(y[e] << 16) * up);
+      q[x][2 * e + 1] = static_cast<_Float16>(__uint_as_float(y[e] & 0xFFFF0000u) * up);
+    }
+  }
+  return __uint_as_float(static_cast<uint32_t>(127 - 8 + ex) << 23);
+}
+
+// Weights p of a block's 8 tokens of this lane (tok + 0 .. 3, tok + 16 .. 19) from its scores acc
+// times c1 plus c2, against the reference m, which follows; l and the numerators o with it.
+template <int NO>
+__device__ __forceinline__ void kv_weigh(f32x4 (&acc)[2], float c1, float c2, float inv, int tok, bool masked, int pos,
+                                         float& m, float& l, f32x4 (&o)[NO], float (&p)[8]) {
+  if (masked) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (tok + (e / 4) * 16 + e % 4 > pos) acc[e / 4][e % 4] = -INFINITY;
+  }
+  // (c1 >= 0: the largest score is that of the largest product)
+  const float mx = fmaf(fmaxf(fmaxf(fmaxf(acc[0][0], acc[0][1]), fmaxf(acc[0][2], acc[0][3])),
+                              fmaxf(fmaxf(acc[1][0], acc[1][1]), fmaxf(acc[1][2], acc[1][3]))), c1, c2);
+  if (__any(mx > m + KV_SLACK)) {
+    const float mn = fmaxf(m, swap_max(mx));
+    const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+#pragma unroll
+    for (int x = 0; x < NO; ++x) o[x] *= al;
+    l *= al;
+    m = mn;
+  }
+  const float off = c2 - (m == -INFINITY ? 0.f : m - KV_UP);
+  float ps = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    p[e] = __builtin_amdgcn_exp2f(fmaf(acc[e / 4][e % 4], c1, off));
+    if (masked && tok + (e / 4) * 16 + e % 4 > pos) p[e] = 0.f;   // (c1 may be 0 or NaN)
+    ps += p[e];
+  }
+  l = ps == 0.f ? l : fmaf(ps, inv, l);   // (a block that the row does not see adds nothing, whatever its scale)
+}
+
 // softmax state of one row: reference, sum, one value of the numerator
 __device__ __forceinline__ void kv_fold(float& m, float& l, float& o, float mp, float lp, float op) {
   const float mn = fmaxf(m, mp);
@@ -518,13 +583,14 @@ struct KvTile {
   int pos0;          // position of the tile's first query
 };
 
-// Tile u of the batch, or false
+// Tile u (of R rows) of the batch, or false
+template <int R>
 __device__ __forceinline__ bool kv_tile(const KvAttendArgs& a, int n, int rep, int64_t u, int h, KvTile& t) {
   int i;
   int64_t k;
   if (a.b.cu) {
-    i = unit_seq(a.b, n, u, rep, 16, 1);
-    k = u - unit_first(a.b, i, rep, 16, 1);
+    i = unit_seq(a.b, n, u, rep, R, 1);
+    k = u - unit_first(a.b, i, rep, R, 1);
   } else {
     const int tiles = (rep + 15) / 16;
     i = static_cast<int>(u / tiles);
@@ -542,9 +608,9 @@ __device__ __forceinline__ bool kv_tile(const KvAttendArgs& a, int n, int rep, i
     return false;
   }
   const int64_t all = static_cast<int64_t>(t.s.n) * rep;
-  if (k * 16 >= all) return false;
-  t.r0 = static_cast<int>(k * 16);
-  t.rows = static_cast<int>(all - t.r0 < 16 ? all - t.r0 : 16);
+  if (k * R >= all) return false;
+  t.r0 = static_cast<int>(k * R);
+  t.rows = static_cast<int>(all - t.r0 < R ? all - t.r0 : R);
   t.pos0 = t.s.len - t.s.n + t.r0 / rep;
   t.nb = (t.s.len - t.s.n + (t.r0 + t.rows - 1) / rep) / KVB + 1;
   return true;
@@ -580,34 +646,7 @@ struct KvWave {
 #pragma unroll
     for (int x = 0; x < KC * 2; ++x)
       qf[x] = __builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(qp + (x / 2) * 64 + (x % 2) * 8));
-    if (BF) {   // the row times a power of two, exact in fp16 (but for values 2^-25 of the row's largest)
-      float mx = 0.f;
-#pragma unroll
-      for (int x = 0; x < KC * 2; ++x) {
-        const uint4 v = __builtin_bit_cast(uint4, qf[x]);
-        const uint32_t y[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          mx = fmaxf(mx, fabsf(__uint_as_float(y[e] << 16)));
-          mx = fmaxf(mx, fabsf(__uint_as_float(y[e] & 0xFFFF0000u)));
-        }
-      }
-      mx = swap_max(mx);
-      int ex = static_cast<int>(__float_as_uint(mx) >> 23) - 127;   // mx in [2^ex, 2^(ex + 1))
-      ex = ex < -100 ? -100 : ex;
-      const float up = __uint_as_float(static_cast<uint32_t>(127 + 8 - ex) << 23);
-      fac *= __uint_as_float(static_cast<uint32_t>(127 - 8 + ex) << 23);
-#pragma unroll
-      for (int x = 0; x < KC * 2; ++x) {
-        const uint4 v = __builtin_bit_cast(uint4, qf[x]);
-        const uint32_t y[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          qf[x][2 * e] = static_cast<_Float16>(__uint_as_float(y[e] << 16) * up);
-          qf[x][2 * e + 1] = static_cast<_Float16>(__uint_as_float(y[e] & 0xFFFF0000u) * up);
-        }
-      }
-    }
+    if (BF) fac *= rows_f16<KC * 2>(qf);
   }
   __device__ __forceinline__ void reset() {
 #pragma unroll
@@ -618,8 +657,7 @@ struct KvWave {
   __device__ __forceinline__ void segment(int seg) {
     const int j = seg * KV_SEG + lane;
     id = 0;
-    ks = 0.f;
-    vs = 1.f;
+    ks = vs = 1.f;
     lv = -INFINITY;
     if (lane < KV_SEG && j < t.nb && (j + 1) * KVB <= t.s.len) {
       id = kv_block(a.c, a.b, t.s.bs + j);
@@ -646,32 +684,8 @@ struct KvWave {
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) kr[x] = *reinterpret_cast<const uint4*>(p + x * 1024 + off);
   }
-  // weights of a block's 8 tokens of this lane, from its scores acc (times c1, plus c2)
-  __device__ __forceinline__ void weigh(const f32x4 (&acc)[2], float c1, float c2, float inv, int tok0, bool masked,
-                                        float (&p)[8]) {
-    float mx = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[e] = fmaf(acc[e / 4][e % 4], c1, c2);
-      if (masked && tok0 + (e / 4) * 16 + g * 4 + e % 4 > pos) p[e] = -INFINITY;
-      mx = fmaxf(mx, p[e]);
-    }
-    if (__any(mx > m + KV_SLACK)) {
-      const float mn = fmaxf(m, swap_max(mx));
-      const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-#pragma unroll
-      for (int x = 0; x < NO; ++x) o[x] *= al;
-      l *= al;
-      m = mn;
-    }
-    const float ref = m == -INFINITY ? 0.f : m - KV_UP;
-    float ps = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
-      ps += p[e];
-    }
-    l = ps == 0.f ? l : fmaf(ps, inv, l);   // (a block that the row does not see adds nothing, whatever its scale)
+  __device__ __forceinline__ void weigh(f32x4 (&acc)[2], float c1, float c2, float inv, int tok0, bool masked, float (&p)[8]) {
+    kv_weigh<NO>(acc, c1, c2, inv, tok0 + g * 4, masked, pos, m, l, o, p);
   }
   // block k of the segment, whose keys load() has read; its values are read while its scores are
   // computed, the keys of block kn while its weights and values are
@@ -830,7 +844,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
     const int64_t u = unit / c.n_kv;
     const int h = static_cast<int>(unit - u * c.n_kv);
     KvTile t;
-    if (!kv_tile(a, n, rep, u, h, t)) continue;
+    if (!kv_tile<16>(a, n, rep, u, h, t)) continue;
     const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
     if (SPLIT && seg0 >= segs) continue;
     const int seg_end = SPLIT || segs == 0 ? seg0 + 1 : segs;
@@ -960,9 +974,13 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
   }
 }
 
-// Folds the segments' states of each tile, in order.
+// Folds the segments' states of each tile, in order.  The factors of a row's fold (a chain of
+// maxima) by one thread per row, JOIN segments at a time, then every thread its values'
+// chain of multiply-adds with the segments' values read ahead.
+constexpr int JOIN = 64;
 template <int HD>
 __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles, int32_t n_seg, int32_t slot_rows) {
+  __shared__ float fx[JOIN][16], fy[JOIN][16], fl[16];
   const KvCache& c = a.c;
   const int n = kv_count(a.b);
   if (n <= 0) return;
@@ -973,17 +991,286 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
   const int64_t tiles = a.b.cu ? unit_first(a.b, n, rep, 16, 1) : static_cast<int64_t>(n) * ((rep + 15) / 16);
   if (u >= tiles || u >= n_tiles) return;
   KvTile t;
-  if (!kv_tile(a, n, rep, u, h, t)) return;
+  if (!kv_tile<16>(a, n, rep, u, h, t)) return;
   const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
   const int64_t step = static_cast<int64_t>(slot_rows) * (HD + 2);
-  for (int e = threadIdx.x; e < t.rows * HD; e += 256) {
+  const float* slot = a.part + unit * n_seg * step;
+  constexpr int PER = 16 * HD / 256;
+  const int used = (t.rows * HD + 255) / 256;   // values of a thread
+  float o[PER], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int x = 0; x < PER; ++x) o[x] = 0.f;
+  for (int s0 = 0; s0 < segs; s0 += JOIN) {
+    const int ns = segs - s0 < JOIN ? segs - s0 : JOIN;
+    __syncthreads();
+    // (reference, sum) of the segments' rows
+    for (int e = threadIdx.x; e < ns * t.rows; e += 256) {
+      const float* ml = slot + (s0 + e / t.rows) * step + slot_rows * HD + 2 * (e % t.rows);
+      fx[e / t.rows][e % t.rows] = ml[0];
+      fy[e / t.rows][e % t.rows] = ml[1];
+    }
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < t.rows) {
+      const int r = threadIdx.x;
+      for (int s = 0; s < ns; ++s) {   // kv_fold's factors and sum
+        const float mp = fx[s][r], lp = fy[s][r], mn = fmaxf(m, mp), ref = mn == -INFINITY ? 0.f : mn;
+        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(mp - ref);
+        l = fmaf(lp, y, l * x);
+        m = mn;
+        fx[s][r] = x;
+        fy[s][r] = y;
+      }
+      fl[r] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      if (x >= used) break;
+      const int e = threadIdx.x + x * 256, r = e / HD < t.rows ? e / HD : 0;
+      const float* p = slot + s0 * step + (e < t.rows * HD ? e : 0);
+      for (int s = 0; s < ns; s += 16) {
+        float v[16];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) v[q] = p[(s + q < ns ? s + q : ns - 1) * step];
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          if (s + q < ns) o[x] = fmaf(v[q], fy[s + q][r], o[x] * fx[s + q][r]);
+      }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int e = threadIdx.x + x * 256;
+    if (e >= t.rows * HD) break;
     const int r = e / HD, d = e % HD, q = t.r0 + r;
-    const float* slot = a.part + unit * n_seg * step;
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int s = 0; s < segs; ++s, slot += step)
-      kv_fold(m, l, o, slot[slot_rows * HD + 2 * r], slot[slot_rows * HD + 2 * r + 1], slot[e]);
-    const float v = l == 0.f ? 0.f : o * (1.0f / l);
+    const float v = segs == 0 || fl[r] == 0.f ? 0.f : o[x] * (1.0f / fl[r]);
     a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
+  }
+}
+
+// ------------------------------------------------------------------ several rows per sequence
+// A workgroup of four waves per 128 query rows of a (sequence, K/V head), 32 rows
+// (two lane-column tiles) per wave, all waves walking the same blocks: a block's bytes
+// become fp16 fragments once per workgroup, in LDS, in the order in which the products
+// take them (every access 16 bytes per lane, in lane order), the next block's bytes in
+// flight meanwhile.  Bound: the softmax's VALU work (16 scores per lane and block of
+// 32 keys, 8 exponentials of 4 issue slots each per tile) beside 32 matrix instructions.
+constexpr int KV_ROWS = 128;
+constexpr int KV_LIST = 64;      // blocks whose numbers and scales are in LDS at a time
+
+template <int HD, bool BF>
+__global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64_t n_tiles) {
+  constexpr int KC = HD / 64, NO = HD / 16, FR = 2 * KC;   // FR fragments of 16 bytes per lane of keys, and of values
+  constexpr int PER = 2 * FR * 64 / 256;                   // of them per thread
+  // [buffer][keys, values][fragment][half][lane] of 8 fp16 (the tail of a bf16 cache: bf16)
+  __shared__ __attribute__((aligned(16))) uint16_t frag[2][2][FR][2][64][8];
+  __shared__ int ids[KV_LIST];
+  __shared__ float kss[KV_LIST], vss[KV_LIST], lvs[KV_LIST];
+  __shared__ int bad[KVB];
+  const KvCache& c = a.c;
+  const int n = kv_count(a.b);
+  if (n <= 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c16 = lane & 15;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rep = a.n_heads / c.n_kv;
+  const int64_t tiles = unit_first(a.b, n, rep, KV_ROWS, 1);
+  const int64_t items = (tiles < n_tiles ? tiles : n_tiles) * c.n_kv;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t u = item / c.n_kv;
+    const int h = static_cast<int>(item - u * c.n_kv);
+    KvTile t;
+    if (!kv_tile<KV_ROWS>(a, n, rep, u, h, t)) continue;
+    const int base = t.s.len - t.s.n;
+    // queries of tile x: row w * 32 + x * 16 + c16
+    const uint16_t* qp[2];
+    half8 qf[2][FR];
+    float fac[2], m[2], l[2];
+    int pos[2];
+    f32x4 o[2][NO];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = w * 32 + x * 16 + c16, row = t.r0 + (r < t.rows ? r : t.rows - 1);
+      pos[x] = base + row / rep;
+      qp[x] = a.q + (t.s.row0 + row / rep) * a.q_ld + (h * rep + row % rep) * HD + g * 16;
+#pragma unroll
+      for (int y = 0; y < FR; ++y) qf[x][y] = __builtin_bit_cast(half8, *reinterpret_cast<const uint4*>(qp[x] + (y / 2) * 64 + (y % 2) * 8));
+      fac[x] = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
+      if (BF) fac[x] *= rows_f16<FR>(qf[x]);
+      m[x] = -INFINITY;
+      l[x] = 0.f;
+#pragma unroll
+      for (int y = 0; y < NO; ++y) o[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // positions of the wave's first and last row: blocks past the last are not its, up to the first all of it is seen
+    const int wr = w * 32 < t.rows ? w * 32 : t.rows - 1, we = w * 32 + 31 < t.rows ? w * 32 + 31 : t.rows - 1;
+    const int first = base + (t.r0 + wr) / rep, last = w * 32 < t.rows ? base + (t.r0 + we) / rep : -1;
+    const int full = t.s.len / KVB < t.nb ? t.s.len / KVB : t.nb;   // the tile's blocks that are not the tail
+    uint4 raw[PER];
+    auto list = [&](int j0) {
+      __syncthreads();
+      if (tid < KV_LIST && j0 + tid < full) {
+        const int id = kv_block(c, a.b, t.s.bs + j0 + tid);
+        ids[tid] = id < 0 ? 0 : id;
+        const int64_t at = static_cast<int64_t>(id < 0 ? 0 : id) * c.n_kv + h;
+        const float v = id < 0 ? 1.f : c.vs[at];
+        kss[tid] = id < 0 ? 1.f : c.ks[at];
+        vss[tid] = 1.0f / v;
+        lvs[tid] = id < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
+      }
+      __syncthreads();
+    };
+    auto load = [&](int j) {
+      const int64_t at = (static_cast<int64_t>(uniform(ids[j % KV_LIST])) * c.n_kv + h) * (KVB * HD);
+#pragma unroll
+      for (int x = 0; x < PER; ++x) {   // fragment (x * 4 + w), keys first
+        const int f = x * 4 + w;
+        raw[x] = *reinterpret_cast<const uint4*>((f < FR ? c.k + at + f * 1024 : c.v + at + (f - FR) * 1024) +
+                                                 static_cast<uint32_t>(lane) * 16);
+      }
+    };
+    auto stage = [&](int buf) {
+#pragma unroll
+      for (int x = 0; x < PER; ++x) {
+        const int f = x * 4 + w;
+        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][0][lane]) = bytes_f16(raw[x].x, raw[x].y);
+        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][1][lane]) = bytes_f16(raw[x].z, raw[x].w);
+      }
+    };
+    list(0);
+    if (full > 0) {
+      load(0);
+      stage(0);
+    }
+    for (int j = 0; j < full; ++j) {
+      const int buf = j & 1;
+      const float ks = kss[j % KV_LIST], inv = vss[j % KV_LIST], lv = lvs[j % KV_LIST];
+      if (j + 1 < full) {
+        if ((j + 1) % KV_LIST == 0) list(j + 1);
+        load(j + 1);
+      }
+      __syncthreads();   // block j staged; the other buffer's block consumed
+      const int tok0 = j * KVB;
+      if (tok0 <= last) {
+        f32x4 acc[2][2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) acc[x][0] = acc[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < FR; ++f)   // tile f / KC of 16 tokens, 64-dim slice f % KC
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const half8 kf = *reinterpret_cast<const half8*>(frag[buf][0][f][e][lane]);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              acc[x][f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][(f % KC) * 2 + e], acc[x][f / KC], 0, 0, 0);
+          }
+        half8 pf[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float p[8];
+          kv_weigh<NO>(acc[x], fac[x] * ks, lv, inv, tok0 + g * 4, tok0 + KVB - 1 > first, pos[x], m[x], l[x], o[x], p);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pf[x][e] = static_cast<_Float16>(p[e]);
+        }
+#pragma unroll
+        for (int f = 0; f < FR; ++f)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const half8 vf = *reinterpret_cast<const half8*>(frag[buf][1][f][e][lane]);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) o[x][2 * f + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[x], o[x][2 * f + e], 0, 0, 0);
+          }
+      }
+      if (j + 1 < full) stage(buf ^ 1);
+    }
+    if (full < t.nb) {   // the tail: its rows as fragments of their own type
+      const int tok0 = full * KVB, left = t.s.len - tok0;
+      const uint16_t* tk = tail_at(c, t.s.tail, 0, h);
+      const uint16_t* tv = tail_at(c, t.s.tail, 1, h);
+      __syncthreads();
+      if (tid < KVB) bad[tid] = 0;
+      __syncthreads();
+      for (int x = tid; x < FR * 2 * 64; x += 256) {
+        const int f = x / 128, e = x / 64 % 2, ln = x % 64, gg = ln >> 4, cc = ln & 15;
+        const int tok = (f / KC) * 16 + cc, row = tok < left ? tok : left - 1;
+        *reinterpret_cast<uint4*>(frag[0][0][f][e][ln]) =
+            *reinterpret_cast<const uint4*>(tk + static_cast<uint32_t>(row * HD + (f % KC) * 64 + gg * 16 + e * 8));
+        union {
+          uint16_t u[8];
+          uint4 q;
+        } v;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const int vt = (y / 4) * 16 + gg * 4 + y % 4, vr = vt < left ? vt : left - 1;
+          v.u[y] = tv[static_cast<uint32_t>(vr * HD + f * 32 + e * 16 + cc)];
+        }
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {   // a later query's infinity or NaN must not meet the weight 0
+          const int vt = (y / 4) * 16 + gg * 4 + y % 4;
+          const bool inf = (v.u[y] & 0x7FFFu) >= (BF ? 0x7F80u : 0x7C00u);
+          if (inf && vt < left) bad[vt] = 1;
+          if (inf || vt >= left) v.u[y] = 0;
+        }
+        *reinterpret_cast<uint4*>(frag[0][1][f][e][ln]) = v.q;
+      }
+      __syncthreads();
+      if (tok0 <= last) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+          for (int f = 0; f < FR; ++f)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint4 kf = *reinterpret_cast<const uint4*>(frag[0][0][f][e][lane]);
+              const int y = (f % KC) * 2 + e;
+              if (BF) {
+                const uint4 qv = *reinterpret_cast<const uint4*>(qp[x] + (y / 2) * 64 + (y % 2) * 8);
+                acc[f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qv), acc[f / KC], 0, 0, 0);
+              } else {
+                acc[f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kf), qf[x][y], acc[f / KC], 0, 0, 0);
+              }
+            }
+          float p[8];
+          kv_weigh<NO>(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, tok0 + g * 4, true, pos[x], m[x],
+                       l[x], o[x], p);
+          union {
+            uint16_t u[8];
+            half8 h;
+            bf16x8 b;
+          } pf;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            pf.u[e] = BF ? f2bf(p[e]) : f2h(p[e]);
+            if (p[e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[x] = __uint_as_float(0x7FC00000u);
+          }
+#pragma unroll
+          for (int f = 0; f < FR; ++f)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint4 vf = *reinterpret_cast<const uint4*>(frag[0][1][f][e][lane]);
+              o[x][2 * f + e] = BF ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf.b, o[x][2 * f + e], 0, 0, 0)
+                                   : __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vf), pf.h, o[x][2 * f + e], 0, 0, 0);
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = w * 32 + x * 16 + c16;
+      const float lw = swap_add(l[x]), inv = lw == 0.f ? 0.f : 1.0f / lw;
+      if (r < t.rows) {
+        const int q = t.r0 + r;
+        uint16_t* op = a.out + (t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + g * 4;
+#pragma unroll
+        for (int y = 0; y < NO; ++y) {
+          uint32_t v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = f2act(o[x][y][e] * inv, a.out_act);
+          *reinterpret_cast<uint2*>(op + y * 16) = make_uint2(v[0] | (v[1] << 16), v[2] | (v[3] << 16));
+        }
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -992,13 +1279,21 @@ struct KvShape {
   int32_t n_seg;     // segments of the longest sequence
   int32_t rows;      // rows of a tile that can be in use
   bool split;
+  bool many;         // many rows per sequence: tiles of KV_ROWS
 };
 static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
   const int rep = n_heads / c.n_kv;
-  KvShape s;
+  KvShape s{};
   s.tiles = b.cu ? b.n_rows * rep / 16 + b.n_seq : static_cast<int64_t>(b.n_seq) * ((rep + 15) / 16);
   s.n_seg = (b.max_len + KV_SEG * KVB - 1) / (KV_SEG * KVB);
   s.rows = b.cu || rep > 16 ? 16 : rep;
+  const int64_t big = b.cu ? b.n_rows * rep / KV_ROWS + b.n_seq : 0;
+  s.many = b.cu && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY && big * c.n_kv >= 256;
+  if (s.many) {
+    s.tiles = big;
+    s.split = false;
+    return s;
+  }
   // segments in workgroups of their own where the tiles alone leave CUs without work
   s.split = s.n_seg > 1 && s.tiles * c.n_kv < 1024 && !b.n_ptr;
   return s;
@@ -1012,15 +1307,26 @@ size_t kv_attend_part_bytes(const KvCache& c, const KvBatch& b, int32_t n_heads)
 
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t s) {
   if (a.b.n_seq == 0 || a.b.n_rows == 0) return hipSuccess;
+  if (a.c.hd != 64 && a.c.hd != 128) return hipErrorInvalidValue;
   const KvShape k = kv_shape(a.c, a.b, a.n_heads);
   if (k.split && !a.part) return hipErrorInvalidValue;
   const int64_t items = k.tiles * a.c.n_kv * (k.split ? k.n_seg : 1);
+  const bool bf = a.c.act == ACT_BF16;
+  if (k.many) {
+    const dim3 grid(static_cast<unsigned>(items < (1 << 20) ? items : 1 << 20));
+#define AIQ_KV_ROWS(HD_, BF_) hipLaunchKernelGGL((k_kv_attend_rows<HD_, BF_>), grid, dim3(256), 0, s, a, k.tiles)
+    if (a.c.hd == 64 && bf) AIQ_KV_ROWS(64, true);
+    else if (a.c.hd == 64) AIQ_KV_ROWS(64, false);
+    else if (bf) AIQ_KV_ROWS(128, true);
+    else AIQ_KV_ROWS(128, false);
+#undef AIQ_KV_ROWS
+    return hipGetLastError();
+  }
   const bool alone = !k.split && items >= KV_ALONE;
   const int64_t cap = !a.b.n_ptr ? 1 << 20 : alone ? 1 << 16 : 1 << 14;   // (a bound from the host only: the sequences may be few)
   const dim3 grid(static_cast<unsigned>(items < cap ? items : cap));
   const int state = alone ? 2 * (a.c.hd + 2) : 4 * (a.c.hd + 2) + (!k.split && k.n_seg > 1 ? a.c.hd + 4 : 0);   // per row
   const size_t lds = static_cast<size_t>(k.rows) * state * 4;
-  const bool bf = a.c.act == ACT_BF16;
 #define AIQ_KV_ATTEND(HD_, BF_, SP_, NW_) \
   hipLaunchKernelGGL((k_kv_attend<HD_, BF_, SP_, NW_>), grid, dim3(64 * NW_), lds, s, a, k.tiles, k.n_seg, k.rows)
 #define AIQ_KV_ATTEND_BF(HD_, BF_)                       \

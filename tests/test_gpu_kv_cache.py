@@ -372,3 +372,56 @@ def test_a_stream_of_its_own():
     out = c.cache.attend(bone, q1, stream=s)
     s.synchronize()
     c.check_attend(c.lens, one, out)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("heads,kv,hd", [(24, 8, 128), (8, 8, 64), (20, 4, 64), (8, 1, 128)])
+def test_attention_of_many_tokens(heads, kv, hd, dtype):
+    """Long prompts on kept ones: ragged, whole, one token among them, none."""
+    say("case: many tokens", heads, kv, hd, dtype)
+    lens = np.array([130, 33, 1, 0, 257, 64, 700, 90, 128, 31] * 4)
+    new = np.minimum(lens, np.array([130, 1, 1, 0, 129, 33, 200, 90, 127, 30] * 4))
+    c = Case(lens, heads, kv, hd, dtype, 21)
+    c.write(lens, lens)
+    out = c.cache.attend(c.batch(lens, new), c.rows("q", lens, new))
+    keep = np.zeros_like(new)
+    keep[:10] = new[:10]
+    c.check_attend(lens, keep, out[:keep.sum()])
+    one = c.cache.attend(c.batch(lens, np.minimum(new, 1)), c.rows("q", lens, np.minimum(new, 1)))   # the last rows by the other kernel
+    at = np.cumsum(new) - 1
+    last = out[torch.as_tensor(at[new > 0]).cuda()]
+    scale = max(float(x.abs().max()) for x in c.v if x.numel())
+    assert float((last.float() - one.float()).abs().max()) <= (2 * U[dtype] + 2.0 ** -13) * scale + 2 * U[dtype] * float(one.float().abs().max())
+
+
+def test_infinity_and_nan_behind_many_queries_stay_there():
+    say("case: NaN behind many queries")
+    for where in (70, 100):
+        c = Case([110] * 40, 4, 2, 64, torch.bfloat16, 22, paged=False)
+        for i in range(0, 40, 2):
+            c.k[i][where:, :, 3], c.v[i][where:, :, 5] = float("nan"), float("inf")
+        lens = np.full(40, 110)
+        c.write(lens, lens)
+        out = c.cache.attend(c.batch(lens, lens), c.rows("q", lens, lens))
+        first = where // 32 * 32 if where < 96 else where
+        sel = np.zeros(40, np.int64)
+        sel[:4] = first
+        c.check_attend(sel, sel, torch.cat([out[i * 110:i * 110 + first] for i in range(4)]))
+        assert torch.isnan(out[where + 1:110]).all() and not torch.isnan(out[110:220]).any()
+
+
+def test_zero_queries_and_keys():
+    """Scores of nothing but zeros: the mean of the values."""
+    say("case: zero queries and keys")
+    for dtype in (torch.float16, torch.bfloat16):
+        for n_seq, new in ((1, 1), (1, 40), (40, 90)):
+            c = Case([90] * n_seq, 4, 2, 64, dtype, 23)
+            for i in range(n_seq):
+                c.k[i][:] = 0
+                c.q[i][:] = 0
+            lens, news = np.full(n_seq, 90), np.full(n_seq, new)
+            c.write(lens, lens)
+            out = c.cache.attend(c.batch(lens, news), c.rows("q", lens, news))
+            sel = np.zeros(n_seq, np.int64)
+            sel[0] = new
+            c.check_attend(lens, sel, out[:new])
