@@ -534,37 +534,65 @@ __device__ __forceinline__ float rows_f16(half8 (&q)[N]) {
   return __uint_as_float(static_cast<uint32_t>(127 - 8 + ex) << 23);
 }
 
-// Weights p of a block's 8 tokens of this lane (tok + 0 .. 3, tok + 16 .. 19) from its scores acc
-// times c1 plus c2, against the reference m, which follows; l and the numerators o with it.
-template <int NO>
-__device__ __forceinline__ void kv_weigh(f32x4 (&acc)[2], float c1, float c2, float inv, int tok, bool masked, int pos,
-                                         float& m, float& l, f32x4 (&o)[NO], float (&p)[8]) {
+// What a block's scales make of its scores: times k, plus the log2 of the values' scale, and that
+// inverted for the sums.  A block with an infinity or NaN has scores of NaN instead (bad), so that
+// tokens that a row does not see can still be masked.
+struct KvScale {
+  float k, log_v, inv_v;
+  bool bad;
+};
+__device__ __forceinline__ KvScale kv_scale(float ks, float vs) {
+  const bool bad = !(ks < INFINITY) || !(vs < INFINITY);
+  return {bad ? 1.f : ks, bad ? 0.f : __builtin_amdgcn_logf(vs), bad || vs == 0.f ? 1.f : 1.0f / vs, bad};
+}
+
+// Scores of NaN for a block that holds one; -infinity for tokens (tok + 0 .. 3, tok + 16 .. 19) past pos.
+__device__ __forceinline__ void kv_mask(f32x4 (&acc)[2], bool bad, bool masked, int tok, int pos) {
+  if (bad) acc[0] = acc[1] = f32x4{NAN, NAN, NAN, NAN};
   if (masked) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (tok + (e / 4) * 16 + e % 4 > pos) acc[e / 4][e % 4] = -INFINITY;
   }
-  // (c1 >= 0: the largest score is that of the largest product)
-  const float mx = fmaf(fmaxf(fmaxf(fmaxf(acc[0][0], acc[0][1]), fmaxf(acc[0][2], acc[0][3])),
-                              fmaxf(fmaxf(acc[1][0], acc[1][1]), fmaxf(acc[1][2], acc[1][3]))), c1, c2);
-  if (__any(mx > m + KV_SLACK)) {
-    const float mn = fmaxf(m, swap_max(mx));
-    const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-#pragma unroll
-    for (int x = 0; x < NO; ++x) o[x] *= al;
-    l *= al;
-    m = mn;
-  }
-  const float off = c2 - (m == -INFINITY ? 0.f : m - KV_UP);
-  float ps = 0.f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    p[e] = __builtin_amdgcn_exp2f(fmaf(acc[e / 4][e % 4], c1, off));
-    if (masked && tok + (e / 4) * 16 + e % 4 > pos) p[e] = 0.f;   // (c1 may be 0 or NaN)
-    ps += p[e];
-  }
-  l = ps == 0.f ? l : fmaf(ps, inv, l);   // (a block that the row does not see adds nothing, whatever its scale)
 }
+
+// The softmax of a block for T tiles of 16 rows, a row per lane column: from the scores acc of this
+// lane's 8 tokens times c1 plus c2 the weights p, against the references m, which follow; the sums l
+// and numerators o with them.
+template <int T, int NO>
+__device__ __forceinline__ void kv_softmax(const f32x4 (&acc)[T][2], const float (&c1)[T], float c2, float inv, float (&m)[T],
+                                           float (&l)[T], f32x4 (&o)[T][NO], float (&p)[T][8]) {
+  float mx[T];
+  bool up = false;
+#pragma unroll
+  for (int x = 0; x < T; ++x) {
+    // (c1 > 0: the largest score is that of the largest product)
+    const f32x4 a = acc[x][0], b = acc[x][1];
+    mx[x] = fmaf(fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]))), c1[x], c2);
+    up = up || mx[x] > m[x] + KV_SLACK;
+  }
+  if (__any(up)) {
+#pragma unroll
+    for (int x = 0; x < T; ++x) {
+      const float mn = fmaxf(m[x], swap_max(mx[x]));
+      const float al = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[x] - mn);
+#pragma unroll
+      for (int y = 0; y < NO; ++y) o[x][y] *= al;
+      l[x] *= al;
+      m[x] = mn;
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < T; ++x) {
+    const float off = c2 - (m[x] == -INFINITY ? 0.f : m[x] - KV_UP);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[x][e] = __builtin_amdgcn_exp2f(fmaf(acc[x][e / 4][e % 4], c1[x], off));
+    const float ps = ((p[x][0] + p[x][1]) + (p[x][2] + p[x][3])) + ((p[x][4] + p[x][5]) + (p[x][6] + p[x][7]));
+    l[x] = fmaf(ps, inv, l[x]);
+  }
+}
+// a factor of scores: positive, so that the product with -infinity is that
+__device__ __forceinline__ float kv_factor(float fac, float ks) { return fmaxf(fac * ks, 0x1p-126f); }
 
 // softmax state of one row: reference, sum, one value of the numerator
 __device__ __forceinline__ void kv_fold(float& m, float& l, float& o, float mp, float lp, float op) {
@@ -630,11 +658,11 @@ struct KvWave {
   float fac;
   half8 qf[KC * 2];
   int id;               // lane x < KV_SEG: the segment's block x, its scales (a number out of bounds: block 0, its
-  float ks, vs, lv;     // tokens weigh nothing); log2 of the values'
+  KvScale sc;           // tokens weigh nothing)
 
   uint4 kr[2 * KC];     // the next block's keys
-  f32x4 o[NO];
-  float m, l;
+  f32x4 o[1][NO];       // (one tile of kv_softmax)
+  float m[1], l[1];
 
   __device__ __forceinline__ KvWave(const KvAttendArgs& a_, const KvTile& t_, int h_, int rep, uint16_t* vt_, int* bad_)
       : a(a_), t(t_), vt(vt_), bad(bad_), h(h_), lane(threadIdx.x & 63), g(lane >> 4), c16(lane & 15) {
@@ -650,22 +678,19 @@ struct KvWave {
   }
   __device__ __forceinline__ void reset() {
 #pragma unroll
-    for (int x = 0; x < NO; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m = -INFINITY;
-    l = 0.f;
+    for (int x = 0; x < NO; ++x) o[0][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[0] = -INFINITY;
+    l[0] = 0.f;
   }
   __device__ __forceinline__ void segment(int seg) {
     const int j = seg * KV_SEG + lane;
     id = 0;
-    ks = vs = 1.f;
-    lv = -INFINITY;
+    sc = {1.f, -INFINITY, 1.f, false};
     if (lane < KV_SEG && j < t.nb && (j + 1) * KVB <= t.s.len) {
       id = kv_block(a.c, a.b, t.s.bs + j);
       if (id >= 0) {
         const int64_t at = static_cast<int64_t>(id) * a.c.n_kv + h;
-        ks = a.c.ks[at];
-        vs = a.c.vs[at];
-        lv = __builtin_amdgcn_logf(vs);
+        sc = kv_scale(a.c.ks[at], a.c.vs[at]);
       }
       id = id < 0 ? 0 : id;
     }
@@ -684,8 +709,10 @@ struct KvWave {
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) kr[x] = *reinterpret_cast<const uint4*>(p + x * 1024 + off);
   }
-  __device__ __forceinline__ void weigh(f32x4 (&acc)[2], float c1, float c2, float inv, int tok0, bool masked, float (&p)[8]) {
-    kv_weigh<NO>(acc, c1, c2, inv, tok0 + g * 4, masked, pos, m, l, o, p);
+  __device__ __forceinline__ void weigh(f32x4 (&acc)[1][2], float c1, float c2, float inv, bool no, int tok0, bool masked, float (&p)[1][8]) {
+    const float c[1] = {c1};
+    kv_mask(acc[0], no, masked, tok0 + g * 4, pos);
+    kv_softmax<1, NO>(acc, c, c2, inv, m, l, o, p);
   }
   // block k of the segment, whose keys load() has read; its values are read while its scores are
   // computed, the keys of block kn while its weights and values are
@@ -697,27 +724,26 @@ struct KvWave {
     const uint32_t off = static_cast<uint32_t>(lane) * 16;
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) vr[x] = *reinterpret_cast<const uint4*>(vp + x * 1024 + off);
-    const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ks), k));
-    const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vs), k));
-    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    auto of = [&](float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), k)); };
+    f32x4 acc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         const uint4 y = kr[tt * KC + kc];
-        acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.x, y.y), qf[kc * 2], acc[tt], 0, 0, 0);
-        acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.z, y.w), qf[kc * 2 + 1], acc[tt], 0, 0, 0);
+        acc[0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.x, y.y), qf[kc * 2], acc[0][tt], 0, 0, 0);
+        acc[0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.z, y.w), qf[kc * 2 + 1], acc[0][tt], 0, 0, 0);
       }
     load(kn);
-    float p[8];
-    weigh(acc, fac * sk, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lv), k)), 1.0f / sv, tok0, tok0 + KVB - 1 > t.pos0, p);
+    float p[1][8];
+    weigh(acc, kv_factor(fac, of(sc.k)), of(sc.log_v), of(sc.inv_v), __builtin_amdgcn_readlane(sc.bad, k) != 0, tok0, tok0 + KVB - 1 > t.pos0, p);
     half8 pf;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pf[e] = static_cast<_Float16>(p[e]);
+    for (int e = 0; e < 8; ++e) pf[e] = static_cast<_Float16>(p[0][e]);
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) {
-      o[2 * x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].x, vr[x].y), pf, o[2 * x], 0, 0, 0);
-      o[2 * x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].z, vr[x].w), pf, o[2 * x + 1], 0, 0, 0);
+      o[0][2 * x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].x, vr[x].y), pf, o[0][2 * x], 0, 0, 0);
+      o[0][2 * x + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].z, vr[x].w), pf, o[0][2 * x + 1], 0, 0, 0);
     }
   }
   // the tail: 16-bit rows, products in their own type; rows past the length are read as the last one, and
@@ -733,7 +759,7 @@ struct KvWave {
     const bool several = a.b.cu != nullptr;
     constexpr int PIECES = HD / 8, PER = KVB * PIECES / 64;
     uint4 kt[4 * KC], vv[PER];
-    f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    f32x4 acc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
     auto load_keys = [&]() {
 #pragma unroll
       for (int x = 0; x < 4 * KC; ++x) {   // token x / (2 KC) * 16 + c16
@@ -774,7 +800,7 @@ struct KvWave {
     }
 #pragma unroll
     for (int x = 0; x < 4 * KC; ++x) {
-      f32x4& s = acc[x / (2 * KC)];
+      f32x4& s = acc[0][x / (2 * KC)];
       const int y = x % (2 * KC);
       if (BF) {
         const uint4 qv = *reinterpret_cast<const uint4*>(qp + (y / 2) * 64 + (y % 2) * 8);
@@ -783,8 +809,8 @@ struct KvWave {
         s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kt[x]), qf[y], s, 0, 0, 0);
       }
     }
-    float p[8];
-    weigh(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, tok0, true, p);
+    float p[1][8];
+    weigh(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, false, tok0, true, p);
     union {
       uint16_t u[8];
       half8 h;
@@ -792,8 +818,8 @@ struct KvWave {
     } pf;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      pf.u[e] = BF ? f2bf(p[e]) : f2h(p[e]);
-      if (several && p[e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l = __uint_as_float(0x7FC00000u);
+      pf.u[e] = BF ? f2bf(p[0][e]) : f2h(p[0][e]);
+      if (several && p[0][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[0] = __uint_as_float(0x7FC00000u);
     }
     // lane 4 a + b of a 16-lane group receives element b of the pieces that lanes a, a + 4, .. address
     lds_u16* const vl = (lds_u16*)(vt);
@@ -807,8 +833,8 @@ struct KvWave {
             reinterpret_cast<lds_v4i16*>(vl + tok * HD + (((d >> 3) ^ (tok & 7)) << 3) + (d & 7)));
       }
       const auto vf = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-      o[x] = BF ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf.b, o[x], 0, 0, 0)
-                : __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vf), pf.h, o[x], 0, 0, 0);
+      o[0][x] = BF ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf.b, o[0][x], 0, 0, 0)
+                   : __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vf), pf.h, o[0][x], 0, 0, 0);
     }
   }
 };
@@ -854,25 +880,25 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
       const int stride = slot_rows * (HD + 2);
       auto fold = [&](bool any, const float* st) {   // the state st (none: !any), then this one, into (x.m, x.l, x.o)
         const float m0 = any ? st[slot_rows * HD + c16] : -INFINITY, l0 = any ? st[slot_rows * HD + slot_rows + c16] : 0.f;
-        const float mn = fmaxf(m0, x.m), ref = mn == -INFINITY ? 0.f : mn;
-        const float e0 = __builtin_amdgcn_exp2f(m0 - ref), e1 = __builtin_amdgcn_exp2f(x.m - ref);
-        x.l = fmaf(x.l, e1, l0 * e0);
+        const float mn = fmaxf(m0, x.m[0]), ref = mn == -INFINITY ? 0.f : mn;
+        const float e0 = __builtin_amdgcn_exp2f(m0 - ref), e1 = __builtin_amdgcn_exp2f(x.m[0] - ref);
+        x.l[0] = fmaf(x.l[0], e1, l0 * e0);
 #pragma unroll
         for (int y = 0; y < NO; ++y) {
           f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
           if (any && c16 < t.rows) z = *reinterpret_cast<const f32x4*>(st + c16 * HD + y * 16 + g * 4);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x.o[y][e] = fmaf(x.o[y][e], e1, z[e] * e0);
+          for (int e = 0; e < 4; ++e) x.o[0][y][e] = fmaf(x.o[0][y][e], e1, z[e] * e0);
         }
-        x.m = mn;
+        x.m[0] = mn;
       };
       auto keep = [&](float* st) {
         if (c16 < t.rows) {
 #pragma unroll
-          for (int y = 0; y < NO; ++y) *reinterpret_cast<f32x4*>(st + c16 * HD + y * 16 + g * 4) = x.o[y];
+          for (int y = 0; y < NO; ++y) *reinterpret_cast<f32x4*>(st + c16 * HD + y * 16 + g * 4) = x.o[0][y];
           if (g == 0) {
-            st[slot_rows * HD + c16] = x.m;
-            st[slot_rows * HD + slot_rows + c16] = x.l;
+            st[slot_rows * HD + c16] = x.m[0];
+            st[slot_rows * HD + slot_rows + c16] = x.l[0];
           }
         }
         wave_sync();
@@ -890,7 +916,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
           for (int k = sh; k < full; k += 4)
             x.take(seg, k, k + 4 < full ? k + 4 : sh < 3 && sh + 1 < full ? sh + 1 : -1);
           if (full < nbs && (full & 3) == sh) x.tail((seg * KV_SEG + full) * KVB);
-          x.l = swap_add(x.l);
+          x.l[0] = swap_add(x.l[0]);
           fold(sh > 0, state);
           if (sh < 3 && sh + 1 < nbs) keep(state);
         }
@@ -899,13 +925,13 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
       }
       if (c16 < t.rows) {
         const int q = t.r0 + c16;
-        const float inv = x.l == 0.f ? 0.f : 1.0f / x.l;
+        const float inv = x.l[0] == 0.f ? 0.f : 1.0f / x.l[0];
         uint16_t* op = a.out + (t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + g * 4;
 #pragma unroll
         for (int y = 0; y < NO; ++y) {
           uint32_t v[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = f2act(x.o[y][e] * inv, a.out_act);
+          for (int e = 0; e < 4; ++e) v[e] = f2act(x.o[0][y][e] * inv, a.out_act);
           *reinterpret_cast<uint2*>(op + y * 16) = make_uint2(v[0] | (v[1] << 16), v[2] | (v[3] << 16));
         }
       }
@@ -920,14 +946,14 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
 #pragma unroll 1
         for (int k = w; k < full; k += 4) x.take(seg, k, k + 4 < full ? k + 4 : -1);
         if (full < nbs && (full & 3) == w) x.tail((seg * KV_SEG + full) * KVB);
-        const float lw = swap_add(x.l);
+        const float lw = swap_add(x.l[0]);
         __syncthreads();   // the last segment's states are read before these are written
         if (c16 < t.rows) {
 #pragma unroll
           for (int y = 0; y < NO; ++y)
-            *reinterpret_cast<f32x4*>(so + (w * slot_rows + c16) * HD + y * 16 + g * 4) = x.o[y];
+            *reinterpret_cast<f32x4*>(so + (w * slot_rows + c16) * HD + y * 16 + g * 4) = x.o[0][y];
           if (g == 0) {
-            sm[w * slot_rows + c16] = x.m;
+            sm[w * slot_rows + c16] = x.m[0];
             sl[w * slot_rows + c16] = lw;
           }
         }
@@ -1056,7 +1082,8 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
 // flight meanwhile.  Bound: the softmax's VALU work (16 scores per lane and block of
 // 32 keys, 8 exponentials of 4 issue slots each per tile) beside 32 matrix instructions.
 constexpr int KV_ROWS = 128;
-constexpr int KV_LIST = 64;      // blocks whose numbers and scales are in LDS at a time
+constexpr int KV_LIST = 64;      // numbers and scales of twice as many blocks are in LDS
+constexpr int KV_AHEAD = 4;      // blocks whose bytes are in flight or staged
 
 template <int HD, bool BF>
 __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64_t n_tiles) {
@@ -1064,8 +1091,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
   constexpr int PER = 2 * FR * 64 / 256;                   // of them per thread
   // [buffer][keys, values][fragment][half][lane] of 8 fp16 (the tail of a bf16 cache: bf16)
   __shared__ __attribute__((aligned(16))) uint16_t frag[2][2][FR][2][64][8];
-  __shared__ int ids[KV_LIST];
-  __shared__ float kss[KV_LIST], vss[KV_LIST], lvs[KV_LIST];
+  __shared__ int ids[2 * KV_LIST];
+  __shared__ KvScale scales[2 * KV_LIST];
   __shared__ int bad[KVB];
   const KvCache& c = a.c;
   const int n = kv_count(a.b);
@@ -1105,49 +1132,47 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
     const int wr = w * 32 < t.rows ? w * 32 : t.rows - 1, we = w * 32 + 31 < t.rows ? w * 32 + 31 : t.rows - 1;
     const int first = base + (t.r0 + wr) / rep, last = w * 32 < t.rows ? base + (t.r0 + we) / rep : -1;
     const int full = t.s.len / KVB < t.nb ? t.s.len / KVB : t.nb;   // the tile's blocks that are not the tail
-    uint4 raw[PER];
-    auto list = [&](int j0) {
-      __syncthreads();
+    uint4 raw[KV_AHEAD][PER];   // the next blocks' bytes
+    auto list = [&](int j0) {   // blocks j0 .. j0 + KV_LIST - 1, in the half of the list whose blocks are long past
       if (tid < KV_LIST && j0 + tid < full) {
-        const int id = kv_block(c, a.b, t.s.bs + j0 + tid);
-        ids[tid] = id < 0 ? 0 : id;
+        const int id = kv_block(c, a.b, t.s.bs + j0 + tid), to = (j0 + tid) % (2 * KV_LIST);
+        ids[to] = id < 0 ? 0 : id;
         const int64_t at = static_cast<int64_t>(id < 0 ? 0 : id) * c.n_kv + h;
-        const float v = id < 0 ? 1.f : c.vs[at];
-        kss[tid] = id < 0 ? 1.f : c.ks[at];
-        vss[tid] = 1.0f / v;
-        lvs[tid] = id < 0 ? -INFINITY : __builtin_amdgcn_logf(v);
+        scales[to] = id < 0 ? KvScale{1.f, -INFINITY, 1.f, false} : kv_scale(c.ks[at], c.vs[at]);
       }
       __syncthreads();
     };
-    auto load = [&](int j) {
-      const int64_t at = (static_cast<int64_t>(uniform(ids[j % KV_LIST])) * c.n_kv + h) * (KVB * HD);
+    auto load = [&](uint4 (&r)[PER], int j) {
+      if (j >= full) return;
+      const int64_t at = (static_cast<int64_t>(uniform(ids[j % (2 * KV_LIST)])) * c.n_kv + h) * (KVB * HD);
 #pragma unroll
       for (int x = 0; x < PER; ++x) {   // fragment (x * 4 + w), keys first
         const int f = x * 4 + w;
-        raw[x] = *reinterpret_cast<const uint4*>((f < FR ? c.k + at + f * 1024 : c.v + at + (f - FR) * 1024) +
-                                                 static_cast<uint32_t>(lane) * 16);
+        r[x] = *reinterpret_cast<const uint4*>((f < FR ? c.k + at + f * 1024 : c.v + at + (f - FR) * 1024) +
+                                               static_cast<uint32_t>(lane) * 16);
       }
     };
-    auto stage = [&](int buf) {
+    auto stage = [&](const uint4 (&r)[PER], int buf) {
 #pragma unroll
       for (int x = 0; x < PER; ++x) {
         const int f = x * 4 + w;
-        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][0][lane]) = bytes_f16(raw[x].x, raw[x].y);
-        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][1][lane]) = bytes_f16(raw[x].z, raw[x].w);
+        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][0][lane]) = bytes_f16(r[x].x, r[x].y);
+        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][1][lane]) = bytes_f16(r[x].z, r[x].w);
       }
     };
     list(0);
-    if (full > 0) {
-      load(0);
-      stage(0);
-    }
+#pragma unroll
+    for (int d = 0; d < KV_AHEAD; ++d) load(raw[d], d);
+    if (full > 0) stage(raw[0], 0);
     for (int j = 0; j < full; ++j) {
-      const int buf = j & 1;
-      const float ks = kss[j % KV_LIST], inv = vss[j % KV_LIST], lv = lvs[j % KV_LIST];
-      if (j + 1 < full) {
-        if ((j + 1) % KV_LIST == 0) list(j + 1);
-        load(j + 1);
-      }
+      const int buf = j & 1, at = j % (2 * KV_LIST);
+      const KvScale sc = scales[at];
+#pragma unroll
+      for (int d = 0; d + 1 < KV_AHEAD; ++d)
+#pragma unroll
+        for (int x = 0; x < PER; ++x) raw[d][x] = raw[d + 1][x];
+      if ((j + KV_AHEAD) % KV_LIST == 0 && j + KV_AHEAD < full) list(j + KV_AHEAD);
+      load(raw[KV_AHEAD - 1], j + KV_AHEAD);
       __syncthreads();   // block j staged; the other buffer's block consumed
       const int tok0 = j * KVB;
       if (tok0 <= last) {
@@ -1164,13 +1189,15 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
               acc[x][f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][(f % KC) * 2 + e], acc[x][f / KC], 0, 0, 0);
           }
         half8 pf[2];
+        float p[2][8];
+        const float c1[2] = {kv_factor(fac[0], sc.k), kv_factor(fac[1], sc.k)};
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float p[8];
-          kv_weigh<NO>(acc[x], fac[x] * ks, lv, inv, tok0 + g * 4, tok0 + KVB - 1 > first, pos[x], m[x], l[x], o[x], p);
+        for (int x = 0; x < 2; ++x) kv_mask(acc[x], uniform(sc.bad) != 0, tok0 + KVB - 1 > first, tok0 + g * 4, pos[x]);
+        kv_softmax<2, NO>(acc, c1, sc.log_v, sc.inv_v, m, l, o, p);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) pf[x][e] = static_cast<_Float16>(p[e]);
-        }
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) pf[x][e] = static_cast<_Float16>(p[x][e]);
 #pragma unroll
         for (int f = 0; f < FR; ++f)
 #pragma unroll
@@ -1180,7 +1207,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
             for (int x = 0; x < 2; ++x) o[x][2 * f + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[x], o[x][2 * f + e], 0, 0, 0);
           }
       }
-      if (j + 1 < full) stage(buf ^ 1);
+      if (j + 1 < full) stage(raw[0], buf ^ 1);
     }
     if (full < t.nb) {   // the tail: its rows as fragments of their own type
       const int tok0 = full * KVB, left = t.s.len - tok0;
@@ -1214,25 +1241,32 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
       }
       __syncthreads();
       if (tok0 <= last) {
+        f32x4 acc[2][2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+          acc[x][0] = acc[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int f = 0; f < FR; ++f)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const uint4 kf = *reinterpret_cast<const uint4*>(frag[0][0][f][e][lane]);
               const int y = (f % KC) * 2 + e;
+              f32x4& s = acc[x][f / KC];
               if (BF) {
                 const uint4 qv = *reinterpret_cast<const uint4*>(qp[x] + (y / 2) * 64 + (y % 2) * 8);
-                acc[f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qv), acc[f / KC], 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qv), s, 0, 0, 0);
               } else {
-                acc[f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kf), qf[x][y], acc[f / KC], 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kf), qf[x][y], s, 0, 0, 0);
               }
             }
-          float p[8];
-          kv_weigh<NO>(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, tok0 + g * 4, true, pos[x], m[x],
-                       l[x], o[x], p);
+        }
+        float p[2][8];
+        const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD)), c1[2] = {scale, scale};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) kv_mask(acc[x], false, true, tok0 + g * 4, pos[x]);
+        kv_softmax<2, NO>(acc, c1, 0.f, 1.f, m, l, o, p);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
           union {
             uint16_t u[8];
             half8 h;
@@ -1240,8 +1274,8 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
           } pf;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            pf.u[e] = BF ? f2bf(p[e]) : f2h(p[e]);
-            if (p[e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[x] = __uint_as_float(0x7FC00000u);
+            pf.u[e] = BF ? f2bf(p[x][e]) : f2h(p[x][e]);
+            if (p[x][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[x] = __uint_as_float(0x7FC00000u);
           }
 #pragma unroll
           for (int f = 0; f < FR; ++f)
