@@ -548,27 +548,41 @@ __device__ __forceinline__ KvScale kv_scale(float ks, float vs) {
 
 // Scores of NaN for a block that holds one; -infinity for tokens (tok + 0 .. 3, tok + 16 .. 19) past pos.
 __device__ __forceinline__ void kv_mask(f32x4 (&acc)[2], bool bad, bool masked, int tok, int pos) {
-  if (bad) acc[0] = acc[1] = f32x4{NAN, NAN, NAN, NAN};
+  if (__builtin_expect(bad, 0)) {
+    asm volatile("");   // a branch, not selects for every block
+    acc[0] = acc[1] = f32x4{NAN, NAN, NAN, NAN};
+  }
   if (masked) {
+    asm volatile("");
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (tok + (e / 4) * 16 + e % 4 > pos) acc[e / 4][e % 4] = -INFINITY;
   }
 }
 
-// The softmax of a block for T tiles of 16 rows, a row per lane column: from the scores acc of this
-// lane's 8 tokens times c1 plus c2 the weights p, against the references m, which follow; the sums l
-// and numerators o with them.
-template <int T, int NO>
-__device__ __forceinline__ void kv_softmax(const f32x4 (&acc)[T][2], const float (&c1)[T], float c2, float inv, float (&m)[T],
-                                           float (&l)[T], f32x4 (&o)[T][NO], float (&p)[T][8]) {
+__device__ __forceinline__ float max3(float a, float b, float c) {   // (fmaxf would quiet its operands first)
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// The softmax of S blocks for T tiles of 16 rows, a row per lane column: from the scores acc of this
+// lane's 8 tokens of each times c1 plus c2 the weights p, against the references m, which follow; the
+// sums l and numerators o with them.
+template <int S, int T, int NO>
+__device__ __forceinline__ void kv_softmax(const f32x4 (&acc)[S][T][2], const float (&c1)[S][T], const float (&c2)[S],
+                                           const float (&inv)[S], float (&m)[T], float (&l)[T], f32x4 (&o)[T][NO],
+                                           float (&p)[S][T][8]) {
   float mx[T];
   bool up = false;
 #pragma unroll
   for (int x = 0; x < T; ++x) {
-    // (c1 > 0: the largest score is that of the largest product)
-    const f32x4 a = acc[x][0], b = acc[x][1];
-    mx[x] = fmaf(fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]))), c1[x], c2);
+    mx[x] = -INFINITY;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {   // (c1 > 0: the largest score is that of the largest product)
+      const f32x4 a = acc[s][x][0], b = acc[s][x][1];
+      mx[x] = fmaxf(mx[x], fmaf(max3(max3(a[0], a[1], a[2]), max3(a[3], b[0], b[1]), fmaxf(b[2], b[3])), c1[s][x], c2[s]));
+    }
     up = up || mx[x] > m[x] + KV_SLACK;
   }
   if (__any(up)) {
@@ -583,13 +597,16 @@ __device__ __forceinline__ void kv_softmax(const f32x4 (&acc)[T][2], const float
     }
   }
 #pragma unroll
-  for (int x = 0; x < T; ++x) {
-    const float off = c2 - (m[x] == -INFINITY ? 0.f : m[x] - KV_UP);
+  for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p[x][e] = __builtin_amdgcn_exp2f(fmaf(acc[x][e / 4][e % 4], c1[x], off));
-    const float ps = ((p[x][0] + p[x][1]) + (p[x][2] + p[x][3])) + ((p[x][4] + p[x][5]) + (p[x][6] + p[x][7]));
-    l[x] = fmaf(ps, inv, l[x]);
-  }
+    for (int x = 0; x < T; ++x) {
+      float (&w)[8] = p[s][x];
+      const float off = c2[s] - (m[x] == -INFINITY ? 0.f : m[x] - KV_UP);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(acc[s][x][e / 4][e % 4], c1[s][x], off));
+      const float ps = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+      l[x] = fmaf(ps, inv[s], l[x]);
+    }
 }
 // a factor of scores: positive, so that the product with -infinity is that
 __device__ __forceinline__ float kv_factor(float fac, float ks) { return fmaxf(fac * ks, 0x1p-126f); }
@@ -709,10 +726,11 @@ struct KvWave {
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) kr[x] = *reinterpret_cast<const uint4*>(p + x * 1024 + off);
   }
-  __device__ __forceinline__ void weigh(f32x4 (&acc)[1][2], float c1, float c2, float inv, bool no, int tok0, bool masked, float (&p)[1][8]) {
-    const float c[1] = {c1};
-    kv_mask(acc[0], no, masked, tok0 + g * 4, pos);
-    kv_softmax<1, NO>(acc, c, c2, inv, m, l, o, p);
+  __device__ __forceinline__ void weigh(f32x4 (&acc)[1][1][2], float c1, float c2, float inv, bool no, int tok0, bool masked,
+                                        float (&p)[1][1][8]) {
+    const float f[1][1] = {{c1}}, add[1] = {c2}, over[1] = {inv};
+    kv_mask(acc[0][0], no, masked, tok0 + g * 4, pos);
+    kv_softmax<1, 1, NO>(acc, f, add, over, m, l, o, p);
   }
   // block k of the segment, whose keys load() has read; its values are read while its scores are
   // computed, the keys of block kn while its weights and values are
@@ -725,21 +743,21 @@ struct KvWave {
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) vr[x] = *reinterpret_cast<const uint4*>(vp + x * 1024 + off);
     auto of = [&](float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), k)); };
-    f32x4 acc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+    f32x4 acc[1][1][2] = {{{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}}};
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc)
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         const uint4 y = kr[tt * KC + kc];
-        acc[0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.x, y.y), qf[kc * 2], acc[0][tt], 0, 0, 0);
-        acc[0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.z, y.w), qf[kc * 2 + 1], acc[0][tt], 0, 0, 0);
+        acc[0][0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.x, y.y), qf[kc * 2], acc[0][0][tt], 0, 0, 0);
+        acc[0][0][tt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(y.z, y.w), qf[kc * 2 + 1], acc[0][0][tt], 0, 0, 0);
       }
     load(kn);
-    float p[1][8];
+    float p[1][1][8];
     weigh(acc, kv_factor(fac, of(sc.k)), of(sc.log_v), of(sc.inv_v), __builtin_amdgcn_readlane(sc.bad, k) != 0, tok0, tok0 + KVB - 1 > t.pos0, p);
     half8 pf;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) pf[e] = static_cast<_Float16>(p[0][e]);
+    for (int e = 0; e < 8; ++e) pf[e] = static_cast<_Float16>(p[0][0][e]);
 #pragma unroll
     for (int x = 0; x < 2 * KC; ++x) {
       o[0][2 * x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(bytes_f16(vr[x].x, vr[x].y), pf, o[0][2 * x], 0, 0, 0);
@@ -759,7 +777,7 @@ struct KvWave {
     const bool several = a.b.cu != nullptr;
     constexpr int PIECES = HD / 8, PER = KVB * PIECES / 64;
     uint4 kt[4 * KC], vv[PER];
-    f32x4 acc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+    f32x4 acc[1][1][2] = {{{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}}};
     auto load_keys = [&]() {
 #pragma unroll
       for (int x = 0; x < 4 * KC; ++x) {   // token x / (2 KC) * 16 + c16
@@ -800,7 +818,7 @@ struct KvWave {
     }
 #pragma unroll
     for (int x = 0; x < 4 * KC; ++x) {
-      f32x4& s = acc[0][x / (2 * KC)];
+      f32x4& s = acc[0][0][x / (2 * KC)];
       const int y = x % (2 * KC);
       if (BF) {
         const uint4 qv = *reinterpret_cast<const uint4*>(qp + (y / 2) * 64 + (y % 2) * 8);
@@ -809,7 +827,7 @@ struct KvWave {
         s = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, kt[x]), qf[y], s, 0, 0, 0);
       }
     }
-    float p[1][8];
+    float p[1][1][8];
     weigh(acc, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), 0.f, 1.f, false, tok0, true, p);
     union {
       uint16_t u[8];
@@ -818,8 +836,8 @@ struct KvWave {
     } pf;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      pf.u[e] = BF ? f2bf(p[0][e]) : f2h(p[0][e]);
-      if (several && p[0][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[0] = __uint_as_float(0x7FC00000u);
+      pf.u[e] = BF ? f2bf(p[0][0][e]) : f2h(p[0][0][e]);
+      if (several && p[0][0][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[0] = __uint_as_float(0x7FC00000u);
     }
     // lane 4 a + b of a 16-lane group receives element b of the pieces that lanes a, a + 4, .. address
     lds_u16* const vl = (lds_u16*)(vt);
@@ -1089,8 +1107,8 @@ template <int HD, bool BF>
 __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64_t n_tiles) {
   constexpr int KC = HD / 64, NO = HD / 16, FR = 2 * KC;   // FR fragments of 16 bytes per lane of keys, and of values
   constexpr int PER = 2 * FR * 64 / 256;                   // of them per thread
-  // [buffer][keys, values][fragment][half][lane] of 8 fp16 (the tail of a bf16 cache: bf16)
-  __shared__ __attribute__((aligned(16))) uint16_t frag[2][2][FR][2][64][8];
+  // [buffer][block][keys, values][fragment][half][lane] of 8 fp16 (the tail of a bf16 cache: bf16)
+  __shared__ __attribute__((aligned(16))) uint16_t frag[2][2][2][FR][2][64][8];
   __shared__ int ids[2 * KV_LIST];
   __shared__ KvScale scales[2 * KV_LIST];
   __shared__ int bad[KVB];
@@ -1134,10 +1152,10 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
     const int full = t.s.len / KVB < t.nb ? t.s.len / KVB : t.nb;   // the tile's blocks that are not the tail
     uint4 raw[KV_AHEAD][PER];   // the next blocks' bytes
     auto list = [&](int j0) {   // blocks j0 .. j0 + KV_LIST - 1, in the half of the list whose blocks are long past
-      if (tid < KV_LIST && j0 + tid < full) {
-        const int id = kv_block(c, a.b, t.s.bs + j0 + tid), to = (j0 + tid) % (2 * KV_LIST);
+      if (tid < KV_LIST) {
+        const int to = (j0 + tid) % (2 * KV_LIST), id = j0 + tid < full ? kv_block(c, a.b, t.s.bs + j0 + tid) : -1;
         ids[to] = id < 0 ? 0 : id;
-        const int64_t at = static_cast<int64_t>(id < 0 ? 0 : id) * c.n_kv + h;
+        const int64_t at = static_cast<int64_t>(id) * c.n_kv + h;
         scales[to] = id < 0 ? KvScale{1.f, -INFINITY, 1.f, false} : kv_scale(c.ks[at], c.vs[at]);
       }
       __syncthreads();
@@ -1152,62 +1170,84 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
                                                static_cast<uint32_t>(lane) * 16);
       }
     };
-    auto stage = [&](const uint4 (&r)[PER], int buf) {
+    auto stage = [&](const uint4 (&r)[PER], int buf, int s) {
 #pragma unroll
       for (int x = 0; x < PER; ++x) {
         const int f = x * 4 + w;
-        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][0][lane]) = bytes_f16(r[x].x, r[x].y);
-        *reinterpret_cast<half8*>(frag[buf][f / FR][f % FR][1][lane]) = bytes_f16(r[x].z, r[x].w);
+        *reinterpret_cast<half8*>(frag[buf][s][f / FR][f % FR][0][lane]) = bytes_f16(r[x].x, r[x].y);
+        *reinterpret_cast<half8*>(frag[buf][s][f / FR][f % FR][1][lane]) = bytes_f16(r[x].z, r[x].w);
       }
     };
     list(0);
 #pragma unroll
-    for (int d = 0; d < KV_AHEAD; ++d) load(raw[d], d);
-    if (full > 0) stage(raw[0], 0);
-    for (int j = 0; j < full; ++j) {
-      const int buf = j & 1, at = j % (2 * KV_LIST);
-      const KvScale sc = scales[at];
+    for (int d = 0; d < KV_AHEAD; ++d) {
 #pragma unroll
-      for (int d = 0; d + 1 < KV_AHEAD; ++d)
+      for (int x = 0; x < PER; ++x) raw[d][x] = make_uint4(0, 0, 0, 0);   // (a pair's second block where there is none: weighs nothing)
+      load(raw[d], d);
+    }
+    stage(raw[0], 0, 0);
+    stage(raw[1], 0, 1);
+    for (int j = 0; j < full; j += 2) {   // blocks j and j + 1
+      const int buf = (j >> 1) & 1;
+      const KvScale sc[2] = {scales[j % (2 * KV_LIST)], scales[(j + 1) % (2 * KV_LIST)]};
 #pragma unroll
-        for (int x = 0; x < PER; ++x) raw[d][x] = raw[d + 1][x];
-      if ((j + KV_AHEAD) % KV_LIST == 0 && j + KV_AHEAD < full) list(j + KV_AHEAD);
-      load(raw[KV_AHEAD - 1], j + KV_AHEAD);
-      __syncthreads();   // block j staged; the other buffer's block consumed
+      for (int d = 0; d + 2 < KV_AHEAD; ++d)
+#pragma unroll
+        for (int x = 0; x < PER; ++x) raw[d][x] = raw[d + 2][x];
+      if ((j + KV_AHEAD) % KV_LIST == 0) list(j + KV_AHEAD);
+      load(raw[KV_AHEAD - 2], j + KV_AHEAD);
+      load(raw[KV_AHEAD - 1], j + KV_AHEAD + 1);
+      __syncthreads();   // blocks j, j + 1 staged; the other buffer's consumed
       const int tok0 = j * KVB;
       if (tok0 <= last) {
-        f32x4 acc[2][2];
+        f32x4 acc[2][2][2];
+        float c1[2][2], p[2][2][8];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) acc[x][0] = acc[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < 2; ++s) {
 #pragma unroll
-        for (int f = 0; f < FR; ++f)   // tile f / KC of 16 tokens, 64-dim slice f % KC
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const half8 kf = *reinterpret_cast<const half8*>(frag[buf][0][f][e][lane]);
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-              acc[x][f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][(f % KC) * 2 + e], acc[x][f / KC], 0, 0, 0);
+          for (int x = 0; x < 2; ++x) {
+            acc[s][x][0] = acc[s][x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            c1[s][x] = kv_factor(fac[x], sc[s].k);
           }
-        half8 pf[2];
-        float p[2][8];
-        const float c1[2] = {kv_factor(fac[0], sc.k), kv_factor(fac[1], sc.k)};
 #pragma unroll
-        for (int x = 0; x < 2; ++x) kv_mask(acc[x], uniform(sc.bad) != 0, tok0 + KVB - 1 > first, tok0 + g * 4, pos[x]);
-        kv_softmax<2, NO>(acc, c1, sc.log_v, sc.inv_v, m, l, o, p);
+          for (int f = 0; f < FR; ++f)   // tile f / KC of 16 tokens, 64-dim slice f % KC
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+            for (int e = 0; e < 2; ++e) {
+              const half8 kf = *reinterpret_cast<const half8*>(frag[buf][s][0][f][e][lane]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) pf[x][e] = static_cast<_Float16>(p[x][e]);
+              for (int x = 0; x < 2; ++x)
+                acc[s][x][f / KC] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][(f % KC) * 2 + e], acc[s][x][f / KC], 0, 0, 0);
+            }
+        }
+        const bool masked = tok0 + 2 * KVB - 1 > first;
 #pragma unroll
-        for (int f = 0; f < FR; ++f)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const half8 vf = *reinterpret_cast<const half8*>(frag[buf][1][f][e][lane]);
+          for (int x = 0; x < 2; ++x) kv_mask(acc[s][x], uniform(sc[s].bad) != 0, masked, tok0 + s * KVB + g * 4, pos[x]);
+        const float c2[2] = {sc[0].log_v, sc[1].log_v}, inv[2] = {sc[0].inv_v, sc[1].inv_v};
+        kv_softmax<2, 2, NO>(acc, c1, c2, inv, m, l, o, p);
+        half8 pf[2][2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) o[x][2 * f + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[x], o[x][2 * f + e], 0, 0, 0);
-          }
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pf[s][x][e] = static_cast<_Float16>(p[s][x][e]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int f = 0; f < FR; ++f)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const half8 vf = *reinterpret_cast<const half8*>(frag[buf][s][1][f][e][lane]);
+#pragma unroll
+              for (int x = 0; x < 2; ++x) o[x][2 * f + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[s][x], o[x][2 * f + e], 0, 0, 0);
+            }
       }
-      if (j + 1 < full) stage(raw[0], buf ^ 1);
+      if (j + 2 < full) {
+        stage(raw[0], buf ^ 1, 0);
+        stage(raw[1], buf ^ 1, 1);
+      }
     }
     if (full < t.nb) {   // the tail: its rows as fragments of their own type
       const int tok0 = full * KVB, left = t.s.len - tok0;
@@ -1219,7 +1259,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
       for (int x = tid; x < FR * 2 * 64; x += 256) {
         const int f = x / 128, e = x / 64 % 2, ln = x % 64, gg = ln >> 4, cc = ln & 15;
         const int tok = (f / KC) * 16 + cc, row = tok < left ? tok : left - 1;
-        *reinterpret_cast<uint4*>(frag[0][0][f][e][ln]) =
+        *reinterpret_cast<uint4*>(frag[0][0][0][f][e][ln]) =
             *reinterpret_cast<const uint4*>(tk + static_cast<uint32_t>(row * HD + (f % KC) * 64 + gg * 16 + e * 8));
         union {
           uint16_t u[8];
@@ -1237,21 +1277,21 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
           if (inf && vt < left) bad[vt] = 1;
           if (inf || vt >= left) v.u[y] = 0;
         }
-        *reinterpret_cast<uint4*>(frag[0][1][f][e][ln]) = v.q;
+        *reinterpret_cast<uint4*>(frag[0][0][1][f][e][ln]) = v.q;
       }
       __syncthreads();
       if (tok0 <= last) {
-        f32x4 acc[2][2];
+        f32x4 acc[1][2][2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          acc[x][0] = acc[x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+          acc[0][x][0] = acc[0][x][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int f = 0; f < FR; ++f)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const uint4 kf = *reinterpret_cast<const uint4*>(frag[0][0][f][e][lane]);
+              const uint4 kf = *reinterpret_cast<const uint4*>(frag[0][0][0][f][e][lane]);
               const int y = (f % KC) * 2 + e;
-              f32x4& s = acc[x][f / KC];
+              f32x4& s = acc[0][x][f / KC];
               if (BF) {
                 const uint4 qv = *reinterpret_cast<const uint4*>(qp[x] + (y / 2) * 64 + (y % 2) * 8);
                 s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qv), s, 0, 0, 0);
@@ -1260,11 +1300,11 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
               }
             }
         }
-        float p[2][8];
-        const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD)), c1[2] = {scale, scale};
+        float p[1][2][8];
+        const float scale = 1.4426950408889634f / sqrtf(static_cast<float>(HD)), c1[1][2] = {{scale, scale}}, none[1] = {0.f}, one[1] = {1.f};
 #pragma unroll
-        for (int x = 0; x < 2; ++x) kv_mask(acc[x], false, true, tok0 + g * 4, pos[x]);
-        kv_softmax<2, NO>(acc, c1, 0.f, 1.f, m, l, o, p);
+        for (int x = 0; x < 2; ++x) kv_mask(acc[0][x], false, true, tok0 + g * 4, pos[x]);
+        kv_softmax<1, 2, NO>(acc, c1, none, one, m, l, o, p);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           union {
@@ -1274,14 +1314,14 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
           } pf;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            pf.u[e] = BF ? f2bf(p[x][e]) : f2h(p[x][e]);
-            if (p[x][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[x] = __uint_as_float(0x7FC00000u);
+            pf.u[e] = BF ? f2bf(p[0][x][e]) : f2h(p[0][x][e]);
+            if (p[0][x][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[x] = __uint_as_float(0x7FC00000u);
           }
 #pragma unroll
           for (int f = 0; f < FR; ++f)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const uint4 vf = *reinterpret_cast<const uint4*>(frag[0][1][f][e][lane]);
+              const uint4 vf = *reinterpret_cast<const uint4*>(frag[0][0][1][f][e][lane]);
               o[x][2 * f + e] = BF ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf), pf.b, o[x][2 * f + e], 0, 0, 0)
                                    : __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vf), pf.h, o[x][2 * f + e], 0, 0, 0);
             }
