@@ -466,7 +466,7 @@ hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, h
 constexpr int KV_SEG = 16;       // blocks per segment
 constexpr float KV_SLACK = 8.0f, KV_UP = 7.0f;
 constexpr int KV_MANY = 48;          // rows per sequence from which on tiles of KV_ROWS take them
-constexpr int64_t KV_ALONE = 4096;   // (tile, K/V head) items from which on waves take them alone
+
 
 __device__ __forceinline__ float swap_max(float v) {   // over the wave's four lane groups
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -1352,7 +1352,7 @@ struct KvShape {
   int64_t tiles;     // bound on the batch's tiles
   int32_t n_seg;     // segments of the longest sequence
   int32_t rows;      // rows of a tile that can be in use
-  bool split;
+  bool split, alone;
   bool many;         // many rows per sequence: tiles of KV_ROWS
 };
 static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
@@ -1365,11 +1365,21 @@ static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
   s.many = b.cu && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY && big * c.n_kv >= 256;
   if (s.many) {
     s.tiles = big;
-    s.split = false;
     return s;
   }
-  // segments in workgroups of their own where the tiles alone leave CUs without work
-  s.split = s.n_seg > 1 && s.tiles * c.n_kv < 1024 && !b.n_ptr;
+  const int64_t items = s.tiles * c.n_kv;
+  // Segments in workgroups of their own where (tile, K/V head) items leave CUs without work for long enough
+  // to pay for the second launch (about 5 us).  Split against one workgroup per item, heads of 64: 8 items of
+  // 800, 1,500 and 4,000 tokens 9.8, 10.4 and 10.4 us against 8.2, 11.6 and 25.4; 64 items of 1,500 10.8 against
+  // 11.8; 256 items of 1,500 and 4,000 18.1 and 29.2 against 16.0 and 34.3 (24/8 heads of 128: 30 and 54
+  // against 23 and 48); 512 items of 4,000 48 against 45.  Among more items only very long
+  // sequences, which a ragged batch may have one of.
+  s.split = !b.n_ptr && ((s.n_seg >= 3 && items < 256) || (s.n_seg >= 16 && items < 1024));
+  // Waves alone where the items fill the chip and none of them is a long chain for its wave.  Alone against a
+  // workgroup per item, heads of 64: 2,048 items of 150 (up to 750) tokens 25.4 us against 19.4, 4,096 32.1 against
+  // 30.3, 8,192 46.8 against 54.2; 2,048 of 30 9.8 against 11.7, of 600 (up to 3,000) 72 against 46; heads of
+  // 128 (groups of 3): 2,048 of 150 34.2 against 35.4, 4,096 48 against 62, 2,048 of 600 139 against 100.
+  s.alone = !s.split && items >= 2048 && items >= static_cast<int64_t>(b.max_len) * (c.hd == 64 ? 6 : 3);
   return s;
 }
 
@@ -1396,16 +1406,15 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t s) {
 #undef AIQ_KV_ROWS
     return hipGetLastError();
   }
-  const bool alone = !k.split && items >= KV_ALONE;
-  const int64_t cap = !a.b.n_ptr ? 1 << 20 : alone ? 1 << 16 : 1 << 14;   // (a bound from the host only: the sequences may be few)
+  const int64_t cap = !a.b.n_ptr ? 1 << 20 : k.alone ? 1 << 16 : 1 << 14;   // (a bound from the host only: the sequences may be few)
   const dim3 grid(static_cast<unsigned>(items < cap ? items : cap));
-  const int state = alone ? 2 * (a.c.hd + 2) : 4 * (a.c.hd + 2) + (!k.split && k.n_seg > 1 ? a.c.hd + 4 : 0);   // per row
+  const int state = k.alone ? 2 * (a.c.hd + 2) : 4 * (a.c.hd + 2) + (!k.split && k.n_seg > 1 ? a.c.hd + 4 : 0);   // per row
   const size_t lds = static_cast<size_t>(k.rows) * state * 4;
 #define AIQ_KV_ATTEND(HD_, BF_, SP_, NW_) \
   hipLaunchKernelGGL((k_kv_attend<HD_, BF_, SP_, NW_>), grid, dim3(64 * NW_), lds, s, a, k.tiles, k.n_seg, k.rows)
 #define AIQ_KV_ATTEND_BF(HD_, BF_)                       \
   if (k.split) AIQ_KV_ATTEND(HD_, BF_, true, 4);         \
-  else if (alone) AIQ_KV_ATTEND(HD_, BF_, false, 1);     \
+  else if (k.alone) AIQ_KV_ATTEND(HD_, BF_, false, 1);     \
   else AIQ_KV_ATTEND(HD_, BF_, false, 4)
   if (a.c.hd == 64 && bf) {
     AIQ_KV_ATTEND_BF(64, true);

@@ -14,7 +14,6 @@ Inputs are plain host structures:
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 
 import numpy as np
@@ -379,6 +378,7 @@ class KvBatch:
         self.struct = struct
         self.keep = keep      # the tensors that the struct points into
         self.n_rows = int(struct.n_rows)
+        self.ws_bytes = {}    # attention workspace by query heads
 
 
 class DeviceKvCache:
@@ -435,13 +435,15 @@ class DeviceKvCache:
 
     def _rows(self, t: torch.Tensor, n_rows: int, heads: int | None, what: str) -> int:
         """Elements between rows of t [n_rows, heads, head_dim]."""
-        _need(t, self.device, self.dtype, what)
-        if t.dim() != 3 or t.shape[0] != n_rows or t.shape[2] != self.head_dim or (heads is not None and t.shape[1] != heads):
-            raise ValueError(f"{what}: [{n_rows}, {heads or 'heads'}, {self.head_dim}] wanted, got {tuple(t.shape)}")
-        if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim)):
+        shape = t.shape
+        if t.device != self.device or t.dtype != self.dtype:
+            raise ValueError(f"{what}: {self.dtype} on {self.device} wanted, got {t.dtype} on {t.device}")
+        if len(shape) != 3 or shape[0] != n_rows or shape[2] != self.head_dim or (heads is not None and shape[1] != heads):
+            raise ValueError(f"{what}: [{n_rows}, {heads or 'heads'}, {self.head_dim}] wanted, got {tuple(shape)}")
+        row, head, one = t.stride()
+        if n_rows and (one != 1 or (shape[1] > 1 and head != self.head_dim)):
             raise ValueError(f"{what}: a row's heads must lie next to each other (strides {t.stride()})")
-        width = t.shape[1] * self.head_dim
-        return t.stride(0) if t.shape[0] > 1 else width
+        return row if n_rows > 1 else shape[1] * self.head_dim
 
     def write(self, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
         """Appends the batch's rows."""
@@ -469,7 +471,9 @@ class DeviceKvCache:
         dtype = out.dtype if out is not None else out_dtype or self.dtype
         if dtype not in (torch.float16, torch.bfloat16):
             raise ValueError(f"out is float16 or bfloat16, not {dtype}")
-        need = B.aiq_kv_attend_workspace_size(self.struct, batch.struct, heads)
+        need = batch.ws_bytes.get(heads)
+        if need is None:
+            need = batch.ws_bytes[heads] = B.aiq_kv_attend_workspace_size(self.struct, batch.struct, heads)
         with _on(self.device, stream) as s:   # the workspace belongs to the stream that uses it
             if out is None:
                 out = torch.empty(q.shape, dtype=dtype, device=self.device)
@@ -479,16 +483,27 @@ class DeviceKvCache:
         return out
 
 
-@contextlib.contextmanager
-def _on(device: torch.device, stream):
+class _on:
     """The device's given or current stream, current while tensors are
-    allocated (they belong to the stream that uses them) and work is enqueued."""
-    with torch.cuda.device(device):
-        if stream is None:
-            yield torch.cuda.current_stream(device).cuda_stream
-        else:
-            with torch.cuda.stream(stream):
-                yield stream.cuda_stream
+    allocated (they belong to the stream that uses them) and work is enqueued;
+    `as` gives its handle."""
+
+    def __init__(self, device: torch.device, stream):
+        self.device, self.stream = device, stream
+
+    def __enter__(self) -> int:
+        self.guards = ()
+        if torch.cuda.current_device() != self.device.index:
+            self.guards = (torch.cuda.device(self.device),)
+        if self.stream is not None:
+            self.guards += (torch.cuda.stream(self.stream),)
+        for g in self.guards:
+            g.__enter__()
+        return (self.stream if self.stream is not None else torch.cuda.current_stream(self.device.index)).cuda_stream
+
+    def __exit__(self, *e):
+        for g in reversed(self.guards):
+            g.__exit__(*e)
 
 
 def _device(device) -> torch.device:
