@@ -87,19 +87,25 @@ __device__ __forceinline__ int kv_count(const KvBatch& b) {
 // Batches with several rows per sequence: sequence i owns the work units from
 // first(i) = per * cu[i] / R + extra * i on, enough for `extra` + its rows / R
 // units; which of them it fills the unit finds out itself.
-__device__ __forceinline__ int64_t unit_first(const KvBatch& b, int i, int per, int R, int extra) {
-  const int at = uniform(b.cu[i]);
+__device__ __forceinline__ int64_t unit_first(const KvBatch& b, int i, int at, int per, int R, int extra) {   // at: cu[i]
   const int64_t c = (at < 0 ? 0 : at) + static_cast<int64_t>(i) * b.n_pre;
   return c * per / R + static_cast<int64_t>(extra) * i;
 }
+__device__ __forceinline__ int64_t unit_first(const KvBatch& b, int i, int per, int R, int extra) {
+  return unit_first(b, i, uniform(b.cu[i]), per, R, extra);
+}
+// The last i with first(i) <= u (the same u for the wave's lanes): 64 places at a time, two rounds of reads
+// for 4,096 sequences where halving takes twelve.
 __device__ __forceinline__ int unit_seq(const KvBatch& b, int n, int64_t u, int per, int R, int extra) {
-  int lo = 0, hi = n;   // the last i with first(i) <= u
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;
   while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (unit_first(b, mid, per, R, extra) <= u)
-      lo = mid;
-    else
-      hi = mid;
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const bool yes = i < hi && unit_first(b, i, b.cu[i < hi ? i : lo], per, R, extra) <= u;
+    const uint64_t past = __ballot(yes);   // (first(lo) <= u: lane 0's at least, where cu is in order)
+    const int k = past ? 63 - __builtin_clzll(past) : 0;
+    lo += k * step;
+    hi = lo + step < hi ? lo + step : hi;
   }
   return lo;
 }
@@ -331,11 +337,25 @@ __global__ __launch_bounds__(256) void k_kv_read(KvMoveArgs a) {
       const uint16_t* tk = tail_at(c, s.tail, 0, h);
       const uint16_t* tv = tail_at(c, s.tail, 1, h);
       const int t0 = j * KVB > before ? j * KVB : before;
-      for (int x = lane; x < (s.len - t0) * (HD / 8); x += 64) {
-        const int t = t0 + x / (HD / 8), e = x % (HD / 8) * 8;
-        const int64_t r = t - before;
-        *reinterpret_cast<uint4*>(ko + r * a.r.k_ld + e) = *reinterpret_cast<const uint4*>(tk + t % KVB * HD + e);
-        *reinterpret_cast<uint4*>(vo + r * a.r.v_ld + e) = *reinterpret_cast<const uint4*>(tv + t % KVB * HD + e);
+      const int pieces = (s.len - t0) * (HD / 8);
+      for (int x0 = 0; x0 < pieces; x0 += 256) {   // four loads of keys and of values in flight
+        auto from = [&](const uint16_t* t, int q) {
+          const int x = x0 + q * 64 + lane < pieces ? x0 + q * 64 + lane : pieces - 1;
+          return *reinterpret_cast<const uint4*>(t + (t0 + x / (HD / 8)) % KVB * HD + x % (HD / 8) * 8);
+        };
+        auto to = [&](int q, const uint4& kk, const uint4& vv) {
+          const int x = x0 + q * 64 + lane, e = x % (HD / 8) * 8;
+          const int64_t r = t0 + x / (HD / 8) - before;
+          if (x >= pieces) return;
+          *reinterpret_cast<uint4*>(ko + r * a.r.k_ld + e) = kk;
+          *reinterpret_cast<uint4*>(vo + r * a.r.v_ld + e) = vv;
+        };
+        const uint4 k0 = from(tk, 0), k1 = from(tk, 1), k2 = from(tk, 2), k3 = from(tk, 3);
+        const uint4 v0 = from(tv, 0), v1 = from(tv, 1), v2 = from(tv, 2), v3 = from(tv, 3);
+        to(0, k0, v0);
+        to(1, k1, v1);
+        to(2, k2, v2);
+        to(3, k3, v3);
       }
       continue;
     }
@@ -1018,13 +1038,14 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
   }
 }
 
-// Folds the segments' states of each tile, in order.  The factors of a row's fold (a chain of
-// maxima) by one thread per row, JOIN segments at a time, then every thread its values'
-// chain of multiply-adds with the segments' values read ahead.
+// Folds the segments' states of each tile, in order, JOIN segments at a time: a wave per row finds how its reference
+// rises (a scan over the segments, a lane each) and the fold's factors, then every thread takes its values'
+// chain of multiply-adds with the first 32 segments' values read ahead.  Bound by the latency of those reads: 23 us for
+// 196 segments of 32 tiles (6.4 MB); with the chain of maxima and exponentials in every thread it took 70.
 constexpr int JOIN = 64;
 template <int HD>
 __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles, int32_t n_seg, int32_t slot_rows) {
-  __shared__ float fx[JOIN][16], fy[JOIN][16], fl[16];
+  __shared__ float fx[JOIN][16], fy[JOIN][16], fl[JOIN][16], top[16], sum[16];
   const KvCache& c = a.c;
   const int n = kv_count(a.b);
   if (n <= 0) return;
@@ -1041,53 +1062,64 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
   const float* slot = a.part + unit * n_seg * step;
   constexpr int PER = 16 * HD / 256;
   const int used = (t.rows * HD + 255) / 256;   // values of a thread
-  float o[PER], m = -INFINITY, l = 0.f;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  float o[PER], l = 0.f;
 #pragma unroll
   for (int x = 0; x < PER; ++x) o[x] = 0.f;
+  if (threadIdx.x < 16) top[threadIdx.x] = -INFINITY;
   for (int s0 = 0; s0 < segs; s0 += JOIN) {
     const int ns = segs - s0 < JOIN ? segs - s0 : JOIN;
+    float v[32];
+    auto read = [&](int x, int s) {   // the segments' values from s on
+      const int e = threadIdx.x + x * 256;
+      const float* p = slot + s0 * step + (e < t.rows * HD ? e : 0);
+#pragma unroll
+      for (int q = 0; q < 32; ++q) v[q] = p[(s + q < ns ? s + q : ns - 1) * step];
+    };
+    read(0, 0);
     __syncthreads();
-    // (reference, sum) of the segments' rows
-    for (int e = threadIdx.x; e < ns * t.rows; e += 256) {
-      const float* ml = slot + (s0 + e / t.rows) * step + slot_rows * HD + 2 * (e % t.rows);
-      fx[e / t.rows][e % t.rows] = ml[0];
-      fy[e / t.rows][e % t.rows] = ml[1];
+    for (int r = w; r < t.rows; r += 4) {   // a wave per row, a lane per segment: the references as they rise, kv_fold's factors
+      const float* ml = slot + (s0 + (lane < ns ? lane : 0)) * step + slot_rows * HD + 2 * r;
+      const float mp = lane < ns ? ml[0] : -INFINITY, lp = ml[1], first = top[r];
+      float m = mp;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const float y = __shfl_up(m, d);
+        m = lane >= d ? fmaxf(m, y) : m;
+      }
+      m = fmaxf(m, first);
+      const float up = __shfl_up(m, 1), before = lane ? up : first, ref = m == -INFINITY ? 0.f : m;
+      fx[lane][r] = __builtin_amdgcn_exp2f(before - ref);
+      fy[lane][r] = __builtin_amdgcn_exp2f(mp - ref);
+      fl[lane][r] = lp;
+      if (lane == 63) top[r] = m;
     }
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < t.rows) {
       const int r = threadIdx.x;
-      for (int s = 0; s < ns; ++s) {   // kv_fold's factors and sum
-        const float mp = fx[s][r], lp = fy[s][r], mn = fmaxf(m, mp), ref = mn == -INFINITY ? 0.f : mn;
-        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(mp - ref);
-        l = fmaf(lp, y, l * x);
-        m = mn;
-        fx[s][r] = x;
-        fy[s][r] = y;
-      }
-      fl[r] = l;
+#pragma unroll 8
+      for (int s = 0; s < ns; ++s) l = fmaf(fl[s][r], fy[s][r], l * fx[s][r]);
+      sum[r] = l;
     }
-    __syncthreads();
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
       if (x >= used) break;
       const int e = threadIdx.x + x * 256, r = e / HD < t.rows ? e / HD : 0;
-      const float* p = slot + s0 * step + (e < t.rows * HD ? e : 0);
-      for (int s = 0; s < ns; s += 16) {
-        float v[16];
+      for (int s = 0; s < ns; s += 32) {
+        if (x > 0 || s > 0) read(x, s);
 #pragma unroll
-        for (int q = 0; q < 16; ++q) v[q] = p[(s + q < ns ? s + q : ns - 1) * step];
-#pragma unroll
-        for (int q = 0; q < 16; ++q)
+        for (int q = 0; q < 32; ++q)
           if (s + q < ns) o[x] = fmaf(v[q], fy[s + q][r], o[x] * fx[s + q][r]);
       }
     }
   }
+  __syncthreads();
 #pragma unroll
   for (int x = 0; x < PER; ++x) {
     const int e = threadIdx.x + x * 256;
     if (e >= t.rows * HD) break;
     const int r = e / HD, d = e % HD, q = t.r0 + r;
-    const float v = segs == 0 || fl[r] == 0.f ? 0.f : o[x] * (1.0f / fl[r]);
+    const float v = segs == 0 || sum[r] == 0.f ? 0.f : o[x] * (1.0f / sum[r]);
     a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
   }
 }
@@ -1362,6 +1394,11 @@ static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
   s.n_seg = (b.max_len + KV_SEG * KVB - 1) / (KV_SEG * KVB);
   s.rows = b.cu || rep > 16 ? 16 : rep;
   const int64_t big = b.cu ? b.n_rows * rep / KV_ROWS + b.n_seq : 0;
+  // Tiles of KV_ROWS rows against tiles of 16, 24/8 heads of 128 and 32/8 heads of 64: 256 sequences of about 300 tokens
+  // with 8 new rows each 89 us against 67 and 49 against 38, with 16 (48 and 64 rows per K/V head) 102 against 115
+  // and 57 against 58, with 32 110 against 174 and 95 against 96; 64 sequences of 900 with 16 71 against 98 and 35
+  // against 52.  Few tiles leave CUs without one: 16 sequences of 2,000 with 16 (176 workgroups) 63 against 46, 4 of
+  // 4,000 with 64 (80) 117 against 81, 16 with 64 (320) 86 against 139.
   s.many = b.cu && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY && big * c.n_kv >= 256;
   if (s.many) {
     s.tiles = big;

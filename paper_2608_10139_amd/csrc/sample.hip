@@ -158,21 +158,30 @@ __device__ __forceinline__ uint64_t block_sum(uint64_t v, SampleSums& s) {
 
 // A workgroup's row: f(logit, id) for every one of this thread's tokens, in
 // ascending order of ids (-infinity past the end); all lanes call f together.
-template <int DT>
+template <int DT, int AHEAD>   // AHEAD: rounds of logits in flight
 struct Row {
   const typename Logits4<DT>::T* p;
   int V, rounds, id0;   // this thread's tokens: id0 + 256 * round + 0 .. 3
   bool inf;             // the maximum is +infinity: its tokens read as 0, the others as -infinity
-  __device__ __forceinline__ void load4(int it, float (&v)[4]) const {
+  typedef typename Logits4<DT>::T T;
+  typedef T Raw __attribute__((ext_vector_type(4)));
+  static constexpr T NONE = DT == AIQ_F32 ? static_cast<T>(-INFINITY) : DT == AIQ_F16 ? static_cast<T>(0xFC00) : static_cast<T>(0xFF80);
+  __device__ __forceinline__ Raw fetch(int it) const {
     const int id = id0 + it * 256;
+    Raw y = {NONE, NONE, NONE, NONE};
     if (__builtin_amdgcn_readfirstlane(id) + 256 <= V) {   // all of the wave's
-      const Logits4<DT> y = *reinterpret_cast<const Logits4<DT>*>(p + id);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = to_logit<DT>(y.v[e]);
+      const Logits4<DT> z = *reinterpret_cast<const Logits4<DT>*>(p + id);
+      y = Raw{z.v[0], z.v[1], z.v[2], z.v[3]};
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = id + e < V ? to_logit<DT>(p[id + e]) : -INFINITY;
+      for (int e = 0; e < 4; ++e)
+        if (id + e < V) y[e] = p[id + e];
     }
+    return y;
+  }
+  __device__ __forceinline__ void values(const Raw& y, float (&v)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = to_logit<DT>(y[e]);
     if (inf) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = v[e] == INFINITY ? 0.f : -INFINITY;
@@ -180,15 +189,18 @@ struct Row {
   }
   template <typename F>
   __device__ __forceinline__ void each4(F f) const {   // f(4 logits, first id)
-    float v[4];
-    load4(0, v);
+    Raw y[AHEAD];   // the next rounds, in flight
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d)
+      if (d < rounds) y[d] = fetch(d);
 #pragma unroll 1
     for (int it = 0; it < rounds; ++it) {
-      float next[4];
-      load4(it + 1 < rounds ? it + 1 : it, next);   // in flight while this round is worked on
-      f(v, id0 + it * 256);
+      float v[4];
+      values(y[0], v);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = next[e];
+      for (int d = 0; d + 1 < AHEAD; ++d) y[d] = y[d + 1];
+      if (it + AHEAD < rounds) y[AHEAD - 1] = fetch(it + AHEAD);
+      f(v, id0 + it * 256);
     }
   }
   template <typename F>
@@ -270,8 +282,8 @@ __device__ __forceinline__ uint64_t share_of(double p, uint64_t total) {
 
 // Moves the threshold (xt, idt) to the token at which the count (MASS: the sum of weights) of the
 // tokens reaches its target: top_k, or top_p of the sum of the tokens kept so far.
-template <int DT, int SW, bool MASS>
-__device__ __forceinline__ void find(const Row<DT>& row, const Weigh& w, double top, float span, float& xt, int& idt, SampleLds<SW>& s) {
+template <int SW, bool MASS, typename R>
+__device__ __forceinline__ void find(const R& row, const Weigh& w, double top, float span, float& xt, int& idt, SampleLds<SW>& s) {
   constexpr int SN = 64 * SW, CAP = cap(SW);
   const int tid = threadIdx.x, lane = tid & 63;
   typedef std::conditional_t<MASS, uint64_t, uint32_t> T;
@@ -402,8 +414,8 @@ __device__ __forceinline__ void sort_keys(uint64_t* key, int n2) {
 // Top-k with what follows it among few tokens: of the 4 maxima that each thread has (of every fourth of its
 // tokens), k lie in the bins up to one, and so at least k tokens do; where they are no more than CAP, the filters and the
 // draw need these alone, sorted.  False: they are more (or fewer maxima than k).
-template <int DT, int SW>
-__device__ __forceinline__ bool draw_few(const Row<DT>& row, const Weigh& w, const float (&most)[4], const SampleArgs& a,
+template <int SW, typename R>
+__device__ __forceinline__ bool draw_few(const R& row, const Weigh& w, const float (&most)[4], const SampleArgs& a,
                                          int64_t r, float u, SampleLds<SW>& s) {
   constexpr int SN = 64 * SW, CAP = cap(SW), PER = CAP / SN > 0 ? CAP / SN : 1;   // sorted tokens per thread
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
@@ -542,7 +554,7 @@ __global__ __launch_bounds__(64 * SW, SW == SW_MAX || FILTER ? 4 : 8) void k_sam
   int64_t rows = a.n_rows;
   if (a.n_ptr && *a.n_ptr < rows) rows = *a.n_ptr;
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    Row<DT> row;
+    Row<DT, SW == SW_MAX || FILTER ? 4 : 2> row;   // (64 registers a lane in the last)
     row.p = static_cast<const typename Logits4<DT>::T*>(a.logits) + r * a.ld;
     row.V = V;
     row.rounds = (V + SN * 4 - 1) / (SN * 4);
@@ -611,12 +623,12 @@ __global__ __launch_bounds__(64 * SW, SW == SW_MAX || FILTER ? 4 : 8) void k_sam
     const float range = w.m - least;
     const float u = a.u[a.u_row ? a.u_row[*a.u_base + a.u_add + r] * a.u_ld + a.u_at : r];
     if constexpr (FILTER) {
-    if (a.top_k > 0 && draw_few<DT, SW>(row, w, most, a, r, u, s)) continue;
-    if (a.top_k > 0) find<DT, SW, false>(row, w, a.top_k, fminf(range, 40.f), xt, idt, s);
+    if (a.top_k > 0 && draw_few<SW>(row, w, most, a, r, u, s)) continue;
+    if (a.top_k > 0) find<SW, false>(row, w, a.top_k, fminf(range, 40.f), xt, idt, s);
     if (a.top_p < 1.0) {
       // tokens with less than (1 - top_p) / V of the maximum's weight are behind the last one kept
       const double far = a.temperature * log(V / (1.0 - a.top_p)) * 1.0001;
-      find<DT, SW, true>(row, w, a.top_p, fminf(range, static_cast<float>(far)), xt, idt, s);
+      find<SW, true>(row, w, a.top_p, fminf(range, static_cast<float>(far)), xt, idt, s);
     }
     }
     // the wave, then the round, then the token that the random number falls into
@@ -650,7 +662,7 @@ __global__ __launch_bounds__(64 * SW, SW == SW_MAX || FILTER ? 4 : 8) void k_sam
     if (target >= at && target - at < mine) {   // this wave's
       for (int it = 0; it < row.rounds; ++it) {
         float v[4];
-        row.load4(it, v);
+        row.values(row.fetch(it), v);
         uint64_t k[4], all = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -682,10 +694,10 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
   if (a.n_rows == 0) return hipSuccess;
   const dim3 grid(static_cast<unsigned>(a.n_rows < 65536 ? a.n_rows : 65536));
   const bool filter = a.temperature > 0.0 && (a.top_k > 0 || a.top_p < 1.0 || a.min_p > 0.0);
-  // 16 waves per row up to the rows that leave CUs without one of theirs, 4 beyond: 512 rows of 32,000 logits 39, 93 and
-  // 42 us (without filters, top-p, top-k) against 53, 121 and 42; 700 rows 54, 135 and 60 against 63, 139 and 45; 1,023
-  // 72, 182 and 81 against 73, 159 and 50.
-  const bool wide = a.n_rows < (filter ? 640 : 1024);
+  // 16 waves per row up to the rows that leave CUs without one of theirs, 4 beyond.  Rows of 32,000 logits, 16 waves
+  // against 4: without filters 512 rows 39 us against 48, 700 rows 52 against 58, 1,023 rows 68 against 71; top-p 512 rows
+  // 91 against 106, 640 rows 129 against 129, 1,023 rows 177 against 155; top-k 512 rows 41 against 36, 640 58 against 38.
+  const bool wide = a.n_rows < (!filter ? 1024 : a.top_k > 0 ? 512 : 640);
 #define AIQ_SAMPLE_K(DT_, SW_, F_) hipLaunchKernelGGL((k_sample<DT_, SW_, F_>), grid, dim3(64 * SW_), 0, s, a)
 #define AIQ_SAMPLE(DT_)                                        \
   if (wide && filter) AIQ_SAMPLE_K(DT_, SW_MAX, true);         \
