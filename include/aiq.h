@@ -580,8 +580,8 @@ typedef struct aiq_kv_cache {
  * len[i] = 0).  Its blocks are entries blk_start[i] .. blk_start[i+1] of
  * blk_ids (blk_ids NULL: entry e is block e), its tail is tail_ids[i] (NULL:
  * i).  Sequences may share full blocks (a common prompt); a block or a tail
- * that a call writes belongs to one sequence alone.  Rows past the last
- * sequence's are not touched.
+ * that a call writes belongs to one sequence alone.  Rows before the first and
+ * past the last sequence's are not touched.
  * A sequence whose numbers do not fit (len[i] above max_len or its blocks, more
  * rows than tokens, a tail or block number out of range) sets
  * AIQ_DEV_KV_RANGE in *status, and nothing of it is read or written out of
@@ -608,8 +608,9 @@ typedef struct aiq_kv_batch {
  * a sequence are in the cache.  Writing a row again has the same result as
  * long as no later block has been begun.
  * Errors: AIQ_EINVAL (NULL pointer, negative count, head_dim, stride or
- * alignment, cu NULL with n_rows != n_seq), AIQ_EUNSUPPORTED (dtype),
- * AIQ_EHIP.  Nothing is enqueued for an empty batch.
+ * alignment, cu NULL with n_rows != n_seq), AIQ_EUNSUPPORTED (dtype; more
+ * than 2^16 heads, 2^26 sequences or 2^30 tokens in one), AIQ_EHIP.  Nothing
+ * is enqueued for an empty batch.
  */
 aiq_status aiq_kv_write(const aiq_kv_cache* cache, const aiq_kv_batch* batch, const void* k, int64_t k_ld,
                         const void* v, int64_t v_ld, void* stream);
@@ -643,8 +644,8 @@ aiq_status aiq_kv_attend_workspace_size(const aiq_kv_cache* cache, const aiq_kv_
  * one row per sequence the result does not depend on the other sequences.
  * workspace: 256-byte aligned, aiq_kv_attend_workspace_size bytes (NULL where
  * that is 0); calls that may overlap need one each.  Errors: AIQ_EINVAL (as
- * aiq_kv_write; n_heads not a multiple of n_kv_heads), AIQ_EUNSUPPORTED
- * (dtype), AIQ_ENOSPC (ws_bytes), AIQ_EHIP.
+ * aiq_kv_write; n_heads not a multiple of n_kv_heads), AIQ_EUNSUPPORTED (as
+ * aiq_kv_write), AIQ_ENOSPC (ws_bytes), AIQ_EHIP.
  */
 aiq_status aiq_kv_attend(const aiq_kv_cache* cache, const aiq_kv_batch* batch, const void* q, int64_t q_ld,
                          int32_t n_heads, void* out, int64_t out_ld, int32_t out_dtype, void* workspace,

@@ -62,6 +62,7 @@ struct aiq_plan {
 namespace {
 
 constexpr size_t ALIGN = 256;
+constexpr int32_t KV_MAX_HEADS = 1 << 16, KV_MAX_SEQ = 1 << 26, KV_MAX_LEN = 1 << 30;   // of an 8-bit cache's batch
 
 bool sampling_ok(const aiq_sampling& s) {
   return s.temperature >= 0.0 && std::isfinite(s.temperature) && s.top_p > 0.0 && s.top_p <= 1.0 && s.min_p >= 0.0 &&
@@ -1130,7 +1131,9 @@ aiq_status aiq_plan_create(const aiq_model* model, const aiq_table* probe, const
     p->gen_blocks = p->gen > 0 ? static_cast<int32_t>((p->seq_ub + GEN_HEAD_ROWS - 1) / GEN_HEAD_ROWS) : 0;
     p->prefix.n = q.n_prefix;
     for (int k = 0; k < q.n_prefix; ++k) p->prefix.tok[k] = q.prefix[k];
-    if (p->kv8 && (kv8_blocks(p) > INT32_MAX || p->t_cap > INT32_MAX)) return fail(AIQ_EUNSUPPORTED);
+    if (p->kv8 && (kv8_blocks(p) > INT32_MAX || p->t_cap > INT32_MAX || p->seq_ub > KV_MAX_SEQ ||
+                   p->max_seq > KV_MAX_LEN - p->gen))
+      return fail(AIQ_EUNSUPPORTED);
     // GROUP BY over any int32 key: at most one group per selected row (by
     // probe column) or per build row (by the joined payload)
     if ((q.agg == AIQ_AGG_AVG_LABEL_COUNT_BY || q.agg == AIQ_AGG_COUNT_BY_PAYLOAD) && q.n_group_keys == 0) {
@@ -1515,6 +1518,8 @@ aiq_status kv_args(const aiq_kv_cache* c, const aiq_kv_batch* b, KvCache* kc, Kv
   if (b->n_seq > 0 && (!b->len || !b->blk_start)) return AIQ_EINVAL;
   if (!b->cu && b->n_rows != b->n_seq) return AIQ_EINVAL;
   if (reinterpret_cast<uintptr_t>(b->status) % 8) return AIQ_EINVAL;
+  // element offsets inside a row, work units and tokens of a sequence are counted in 32 bits
+  if (c->n_kv_heads > KV_MAX_HEADS || b->n_seq > KV_MAX_SEQ || b->max_len > KV_MAX_LEN) return AIQ_EUNSUPPORTED;
   kc->k = static_cast<uint8_t*>(c->k);
   kc->v = static_cast<uint8_t*>(c->v);
   kc->ks = c->k_scale;
@@ -1576,6 +1581,7 @@ aiq_status aiq_kv_attend_workspace_size(const aiq_kv_cache* cache, const aiq_kv_
   const aiq_status e = kv_args(cache, batch, &c, &b);
   if (e != AIQ_OK) return e;
   if (!bytes || n_heads <= 0 || n_heads % c.n_kv) return AIQ_EINVAL;
+  if (n_heads > KV_MAX_HEADS) return AIQ_EUNSUPPORTED;
   *bytes = kv_attend_part_bytes(c, b, n_heads);
   return AIQ_OK;
 }
@@ -1587,6 +1593,7 @@ aiq_status aiq_kv_attend(const aiq_kv_cache* cache, const aiq_kv_batch* batch, c
   const aiq_status e = kv_args(cache, batch, &a.c, &a.b);
   if (e != AIQ_OK) return e;
   if (n_heads <= 0 || n_heads % a.c.n_kv) return AIQ_EINVAL;
+  if (n_heads > KV_MAX_HEADS) return AIQ_EUNSUPPORTED;
   if (out_dtype != AIQ_F16 && out_dtype != AIQ_BF16) return AIQ_EUNSUPPORTED;
   const int64_t width = static_cast<int64_t>(n_heads) * a.c.hd;
   if (a.b.n_rows > 0 && (!kv_rows_ok(q, q_ld, width) || !kv_rows_ok(out, out_ld, width))) return AIQ_EINVAL;

@@ -180,7 +180,9 @@ __device__ __forceinline__ bool move_unit(const KvCache& c, const KvBatch& b, in
   jj = 0;
   if (b.cu) {
     i = unit_seq(b, n, u, 1, KVB, 2);
-    jj = static_cast<int>(u - unit_first(b, i, 1, KVB, 2));
+    const int64_t d = u - unit_first(b, i, 1, KVB, 2);
+    if (d < 0) return false;   // rows before the first sequence's
+    jj = static_cast<int>(d);
   }
   return kv_seq(c, b, i, s);
 }
@@ -673,7 +675,7 @@ __device__ __forceinline__ bool kv_tile(const KvAttendArgs& a, int n, int rep, i
     return false;
   }
   const int64_t all = static_cast<int64_t>(t.s.n) * rep;
-  if (k * R >= all) return false;
+  if (k < 0 || k * R >= all) return false;   // (k < 0: rows before the first sequence's)
   t.r0 = static_cast<int>(k * R);
   t.rows = static_cast<int>(all - t.r0 < R ? all - t.r0 : R);
   t.pos0 = t.s.len - t.s.n + t.r0 / rep;

@@ -377,6 +377,7 @@ class KvBatch:
     def __init__(self, struct: B.aiq_kv_batch, keep: tuple):
         self.struct = struct
         self.keep = keep      # the tensors that the struct points into
+        self.device = keep[0].device
         self.n_rows = int(struct.n_rows)
         self.ws_bytes = {}    # attention workspace by query heads
 
@@ -433,6 +434,12 @@ class DeviceKvCache:
         b.status = _ptr(self.status)
         return KvBatch(b, (length, blk_start, cu, blk_ids, tail_ids))
 
+    def _mine(self, batch: KvBatch) -> int:
+        """The batch's rows; its tensors must be on the cache's device."""
+        if batch.device != self.device:
+            raise ValueError(f"batch: one on {self.device} wanted, got one on {batch.device}")
+        return batch.n_rows
+
     def _rows(self, t: torch.Tensor, n_rows: int, heads: int | None, what: str) -> int:
         """Elements between rows of t [n_rows, heads, head_dim]."""
         shape = t.shape
@@ -447,15 +454,16 @@ class DeviceKvCache:
 
     def write(self, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
         """Appends the batch's rows."""
-        ks, vs = (self._rows(t, batch.n_rows, self.n_kv_heads, w) for t, w in ((k, "k"), (v, "v")))
+        n = self._mine(batch)
+        ks, vs = (self._rows(t, n, self.n_kv_heads, w) for t, w in ((k, "k"), (v, "v")))
         with _on(self.device, stream) as s:
             B.aiq_kv_write(self.struct, batch.struct, _ptr(k), ks, _ptr(v), vs, s)
 
     def read(self, batch: KvBatch, stream=None) -> tuple:
         """The batch's rows as the cache holds them: (k, v)."""
-        w = self.n_kv_heads * self.head_dim
+        n, w = self._mine(batch), self.n_kv_heads * self.head_dim
         with _on(self.device, stream) as s:
-            k, v = (torch.empty((batch.n_rows, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device)
+            k, v = (torch.empty((n, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device)
                     for _ in range(2))
             B.aiq_kv_read(self.struct, batch.struct, _ptr(k), w, _ptr(v), w, s)
         return k, v
@@ -464,7 +472,7 @@ class DeviceKvCache:
                out_dtype: torch.dtype | None = None, stream=None) -> torch.Tensor:
         """Attention of the batch's rows q [rows, heads, head_dim] over the
         cache (their own tokens included), in out_dtype (default the cache's)."""
-        qs = self._rows(q, batch.n_rows, None, "q")
+        qs = self._rows(q, self._mine(batch), None, "q")
         heads = q.shape[1]
         if out is not None and (out.shape != q.shape or not out.is_contiguous() or out.device != self.device):
             raise ValueError(f"out: contiguous {tuple(q.shape)} on {self.device} wanted")
@@ -489,6 +497,8 @@ class _on:
     `as` gives its handle."""
 
     def __init__(self, device: torch.device, stream):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream: one of {device} wanted, got one of {stream.device}")
         self.device, self.stream = device, stream
 
     def __enter__(self) -> int:

@@ -425,3 +425,75 @@ def test_zero_queries_and_keys():
             sel = np.zeros(n_seq, np.int64)
             sel[0] = new
             c.check_attend(lens, sel, out[:new])
+
+
+@pytest.mark.parametrize("lead", [1, 40, 300])
+@pytest.mark.parametrize("lens,new", [([70, 200, 33], [3, 40, 1]), ([300] * 40, [90] * 40)])
+def test_rows_before_the_first_sequence_are_left_alone(lens, new, lead):
+    # the call's rows start at cu[0] > 0: what lies before belongs to nobody, in the cache and in the outputs
+    say("lead", lead, len(lens))
+    c = Case(lens, 8, 8, 64, torch.float16, 31)
+    old = [L - m for L, m in zip(lens, new)]
+    c.write(old, old)
+    at = starts(new) + lead
+    n = int(at[-1])
+
+    def behind(x):
+        y = torch.full((n,) + x.shape[1:], 3.0, dtype=x.dtype, device="cuda")
+        y[lead:] = x
+        return y
+
+    b = c.cache.batch(i32(lens), c.blk_start, max(lens), cu=i32(at), blk_ids=c.blk_ids, tail_ids=c.tail_ids)
+    c.cache.write(b, behind(c.rows("k", lens, new)), behind(c.rows("v", lens, new)))
+    c.check_read(lens)
+    out = torch.full((n, 8, 64), 5.0, dtype=torch.float16, device="cuda")
+    c.cache.attend(b, behind(c.rows("q", lens, new)), out=out)
+    assert bool((out[:lead] == 5.0).all())
+    c.check_attend(lens, new, out[lead:])
+    k = torch.full((n, 8, 64), 5.0, dtype=torch.float16, device="cuda")
+    v = k.clone()
+    B.aiq_kv_read(c.cache.struct, b.struct, k.data_ptr(), 512, v.data_ptr(), 512, torch.cuda.current_stream().cuda_stream)
+    for got, what in ((k, 0), (v, 1)):
+        assert bool((got[:lead] == 5.0).all())
+        for i, (L, m) in enumerate(zip(lens, new)):
+            want = torch.from_numpy(c.held(i, L)[what][L - m:]).to(torch.float32).half()
+            assert torch.equal(got[at[i]:at[i + 1]].cpu(), want)
+    c.ok()
+
+
+def test_two_streams_and_two_graphs_at_once():
+    # long sequences of one cache, split between workgroups: each call has a workspace of its own
+    say("two streams")
+    a, b = Case([9000, 5000, 700], 8, 8, 64, torch.float16, 41), Case([4000, 20000], 24, 8, 128, torch.bfloat16, 42)
+    calls = []
+    for c in (a, b):
+        lens, ones = list(c.lens), [1] * len(c.lens)
+        c.write(lens, lens)
+        calls.append((c.cache, c.batch(lens, ones, single=True), c.rows("q", lens, ones)))
+    want = [cache.attend(batch, q) for cache, batch, q in calls]
+    for c, w in zip((a, b), want):
+        c.check_attend(list(c.lens), [1] * len(c.lens), w)
+    assert all(batch.ws_bytes[q.shape[1]] > 0 for _, batch, q in calls)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        got = [cache.attend(batch, q, stream=s) for (cache, batch, q), s in zip(calls, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+    say("two graphs")
+    graphs, outs = [], []
+    for (cache, batch, q), s in zip(calls, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(cache.attend(batch, q))
+        graphs.append(g)
+    for _ in range(4):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = calls[0][0].attend(*calls[0][1:])
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want)) and torch.equal(eager, want[0])

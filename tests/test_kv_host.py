@@ -2,6 +2,7 @@
 a device: a bad call returns its status before anything is enqueued (fake
 addresses are never read)."""
 import ctypes as C
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -60,6 +61,20 @@ def test_bad_caches(kw, code):
 @pytest.mark.parametrize("kw", BAD_BATCH, ids=str)
 def test_bad_batches(kw):
     assert write(cache(), batch(**kw)) == write(cache(), batch(**kw), read=True) == attend(cache(), batch(**kw)) == B.AIQ_EINVAL
+
+
+def test_counts_past_32_bits_are_refused():
+    n = C.c_size_t()
+    size = B.load().aiq_kv_attend_workspace_size
+    for c, b, heads in ((cache(n_kv_heads=(1 << 16) + 1), batch(), (1 << 16) + 1), (cache(), batch(max_len=(1 << 30) + 1), 8),
+                        (cache(), batch(n_seq=(1 << 26) + 1), 8)):
+        ld = 1 << 30
+        assert write(c, b, k_ld=ld, v_ld=ld) == write(c, b, k_ld=ld, v_ld=ld, read=True) == B.AIQ_EUNSUPPORTED
+        assert attend(c, b, q_ld=ld, out_ld=ld, heads=heads) == B.AIQ_EUNSUPPORTED
+        assert size(C.byref(c), C.byref(b), heads, C.byref(n)) == B.AIQ_EUNSUPPORTED
+    assert attend(cache(), batch(), q_ld=1 << 30, out_ld=1 << 30, heads=(1 << 16) + 2) == B.AIQ_EUNSUPPORTED
+    assert size(C.byref(cache()), C.byref(batch()), (1 << 16) + 2, C.byref(n)) == B.AIQ_EUNSUPPORTED
+    assert size(C.byref(cache()), C.byref(batch(max_len=1 << 30)), 1 << 16, C.byref(n)) == B.AIQ_OK
 
 
 @pytest.mark.parametrize("kw", [dict(k=0), dict(v=0), dict(k=FAKE + 2), dict(v=FAKE + 8), dict(k_ld=127), dict(v_ld=120),
@@ -150,6 +165,20 @@ def test_wrapper_refusals():
             sample(*args)
 
 
+def test_wrapper_refuses_other_devices():
+    c = DeviceKvCache(4, 2, 2, 64, device="cpu")
+    i = lambda *x: torch.tensor(x, dtype=torch.int32)   # noqa: E731
+    b, rows = c.batch(i(5, 6), i(0, 2, 4), 64), torch.zeros(2, 2, 64, dtype=torch.float16)
+    other = SimpleNamespace(device=torch.device("cuda", 1))
+    for call in (lambda s: c.write(b, rows, rows, stream=s), lambda s: c.read(b, stream=s), lambda s: c.attend(b, rows, stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            call(other)
+    b.device = torch.device("cuda", 1)
+    for call in (lambda: c.write(b, rows, rows), lambda: c.read(b), lambda: c.attend(b, rows)):
+        with pytest.raises(ValueError, match="batch"):
+            call()
+
+
 def gen_query(**kw):
     q = query(gen_tokens=4, eos_id=-1)
     for k, v in kw.items():
@@ -184,3 +213,16 @@ def test_cache_types_of_a_plan():
     assert plan(gen_query(), kv_dtype=B.AIQ_BF16) == plan(gen_query(), kv_dtype=-1) == B.AIQ_EINVAL
     assert plan(query(), kv_dtype=B.AIQ_I8) == B.AIQ_EINVAL   # nothing is generated
     assert plan(query(), kv_dtype=B.AIQ_F16) == B.AIQ_OK
+
+
+def test_8_bit_plans_out_of_range():
+    def status(q=None, t=None, **m):
+        o = B.aiq_plan_opts()
+        o.kv_dtype = B.AIQ_I8
+        return B.aiq_plan_create_status(model(**m), t or table(), None, q or gen_query(), o)
+
+    assert status() == B.AIQ_OK
+    assert status(d_model=256) != B.AIQ_OK   # heads of 32
+    t = table()
+    t.max_list_len = (1 << 31) - 2           # lengths and generated tokens pass 32 bits
+    assert status(t=t) == B.AIQ_EUNSUPPORTED
