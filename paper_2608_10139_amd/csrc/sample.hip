@@ -187,8 +187,13 @@ struct Row {
       for (int e = 0; e < 4; ++e) v[e] = v[e] == INFINITY ? 0.f : -INFINITY;
     }
   }
+  struct Ids {
+    int first;
+    __device__ __forceinline__ int operator[](int e) const { return first + e; }
+  };
+  static constexpr bool FEW = false;
   template <typename F>
-  __device__ __forceinline__ void each4(F f) const {   // f(4 logits, first id)
+  __device__ __forceinline__ void each4(F f) const {   // f(4 logits, their ids)
     Raw y[AHEAD];   // the next rounds, in flight
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d)
@@ -200,15 +205,26 @@ struct Row {
 #pragma unroll
       for (int d = 0; d + 1 < AHEAD; ++d) y[d] = y[d + 1];
       if (it + AHEAD < rounds) y[AHEAD - 1] = fetch(it + AHEAD);
-      f(v, id0 + it * 256);
+      f(v, Ids{id0 + it * 256});
     }
   }
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    each4([&](const float (&v)[4], int id) {
+    each4([&](const float (&v)[4], const Ids& id) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f(v[e], id + e);
+      for (int e = 0; e < 4; ++e) f(v[e], id[e]);
     });
+  }
+};
+
+// Tokens gathered from a row, up to 4 per thread (an empty place: -infinity, behind every threshold).
+struct List {
+  static constexpr bool FEW = true;   // no more than CAP
+  float x[4];
+  int id[4];
+  template <typename F>
+  __device__ __forceinline__ void each4(F f) const {
+    f(x, id);
   }
 };
 
@@ -293,10 +309,10 @@ __device__ __forceinline__ void find(const R& row, const Weigh& w, double top, f
   if (tid == 0) s.n = 0;
   __syncthreads();
   T rest = 0;   // the last bin's
-  row.each4([&](const float (&x)[4], int id) {
+  row.each4([&](const float (&x)[4], const auto& id) {
     bool in[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) in[e] = upto(x[e], id + e, xt, idt);
+    for (int e = 0; e < 4; ++e) in[e] = upto(x[e], id[e], xt, idt);
     if (!__any(in[0] || in[1] || in[2] || in[3])) return;
     T v[4];
 #pragma unroll
@@ -327,17 +343,17 @@ __device__ __forceinline__ void find(const R& row, const Weigh& w, double top, f
     const float f = bins.place(x);
     return f >= from && f < to && upto(x, id, xt, idt);
   };
-  row.each4([&](const float (&x)[4], int id) {
+  row.each4([&](const float (&x)[4], const auto& id) {
     bool in[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) in[e] = in_bin(x[e], id + e);
+    for (int e = 0; e < 4; ++e) in[e] = in_bin(x[e], id[e]);
     if (!__any(in[0] || in[1] || in[2] || in[3])) return;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) gather(in[e], x[e], id + e, s);
+    for (int e = 0; e < 4; ++e) gather(in[e], x[e], id[e], s);
   });
   __syncthreads();
   const int n = s.n;
-  if (n <= CAP) {
+  if (R::FEW || n <= CAP) {
     for (int i = tid; MASS && i < n; i += SN) s.w[i] = w.of(key_logit(s.key[i]));
     __syncthreads();
     int each = 64;   // threads per token
@@ -352,7 +368,7 @@ __device__ __forceinline__ void find(const R& row, const Weigh& w, double top, f
       ahead += before;
       if (i < n && tid % each == 0 && ahead < target && target <= ahead + (MASS ? s.w[i] : 1)) s.last = key;
     }
-  } else {
+  } else if constexpr (!R::FEW) {
     // the largest key K such that the bin's tokens with keys from K on reach the target, bit by bit
     uint32_t K = 0;
     for (int bit = 31; bit >= 0; --bit) {
@@ -394,31 +410,14 @@ __device__ __forceinline__ uint64_t draw_target(float u, uint64_t total) {
   return g < total ? g : total - 1;
 }
 
-// Sorts the first `n2` (a power of two) keys, the largest first.
-template <int SW>
-__device__ __forceinline__ void sort_keys(uint64_t* key, int n2) {
-  for (int k = 2; k <= n2; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int i = threadIdx.x; i < n2 / 2; i += 64 * SW) {
-        const int a = 2 * i - (i & (j - 1)), b = a + j;   // i's pair at distance j
-        const uint64_t x = key[a], y = key[b];
-        if ((a & k) == 0 ? x < y : x > y) {
-          key[a] = y;
-          key[b] = x;
-        }
-      }
-      __syncthreads();
-    }
-}
-
 // Top-k with what follows it among few tokens: of the 4 maxima that each thread has (of every fourth of its
 // tokens), k lie in the bins up to one, and so at least k tokens do; where they are no more than CAP, the filters and the
-// draw need these alone, sorted.  False: they are more (or fewer maxima than k).
+// draw need these alone.  False: they are more (or fewer maxima than k).
 template <int SW, typename R>
 __device__ __forceinline__ bool draw_few(const R& row, const Weigh& w, const float (&most)[4], const SampleArgs& a,
                                          int64_t r, float u, SampleLds<SW>& s) {
-  constexpr int SN = 64 * SW, CAP = cap(SW), PER = CAP / SN > 0 ? CAP / SN : 1;   // sorted tokens per thread
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  constexpr int SN = 64 * SW, CAP = cap(SW), PER = CAP / SN;   // gathered tokens per thread
+  const int tid = threadIdx.x;
   uint32_t* bin = reinterpret_cast<uint32_t*>(s.bin);
   const Bins bins(w.m, 32.f);
   for (int b = tid; b < BINS; b += SN) bin[b] = 0;
@@ -435,13 +434,13 @@ __device__ __forceinline__ bool draw_few(const R& row, const Weigh& w, const flo
   const int at = s.at;
   if (at < 0 || at == BINS - 1) return false;
   const float to = static_cast<float>(at + 1);
-  row.each4([&](const float (&x)[4], int id) {
+  row.each4([&](const float (&x)[4], const auto& id) {
     bool in[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) in[e] = (w.m - x[e]) * bins.per < to;
     if (!__any(in[0] || in[1] || in[2] || in[3])) return;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) gather(in[e], x[e], id + e, s);
+    for (int e = 0; e < 4; ++e) gather(in[e], x[e], id[e], s);
   });
   __syncthreads();
   const int n = s.n;
@@ -478,68 +477,51 @@ __device__ __forceinline__ bool draw_few(const R& row, const Weigh& w, const flo
     __syncthreads();
     return true;
   }
-  int n2 = 256;
-  while (n2 < n) n2 <<= 1;
-  for (int i = n + tid; i < n2; i += SN) s.key[i] = 0;
-  __syncthreads();
-  sort_keys<SW>(s.key, n2);
-  // weights in order, and their running sums
-  uint64_t v[PER], mine = 0;
+  // the same steps as over a row, with the tokens in registers
+  static_assert(PER >= 1 && PER <= 4);
+  List list;
 #pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    const int i = tid * PER + q;
-    v[q] = i < k ? w.of(key_logit(s.key[i])) : 0;
-    mine += v[q];
-  }
-  auto scan = [&](uint64_t x, uint64_t& total) {   // of the threads before this one
-    const uint64_t incl = wave_scan_u64(x);
-    __syncthreads();
-    if (lane == 63) s.wave[wv] = incl;
-    __syncthreads();
-    uint64_t before = incl - x;
-    total = 0;
-#pragma unroll
-    for (int y = 0; y < SW; ++y) {
-      if (y < wv) before += s.wave[y];
-      total += s.wave[y];
-    }
-    return before;
-  };
-  uint64_t total;
-  uint64_t ahead = scan(mine, total);
-  const uint64_t target = a.top_p < 1.0 ? share_of(a.top_p, total) : total;
-  uint64_t keep[PER], id_key[PER];
-#pragma unroll
-  for (int q = 0; q < PER; ++q) {   // kept: those before the sum reaches the target
-    const int i = tid * PER + q;
-    const bool in = i < k && ahead < target;
-    keep[q] = in ? w.kept(key_logit(s.key[i])) : 0;
-    id_key[q] = in ? (s.key[i] << 32) | static_cast<uint32_t>(i) : 0;   // (~id, place): the lowest id is the largest
-    ahead += v[q];
+  for (int q = 0; q < 4; ++q) {
+    const int i = tid + q * SN;
+    const bool is = q < PER && i < n;
+    const uint64_t key = is ? s.key[i] : 0;
+    list.x[q] = is ? key_logit(key) : -INFINITY;
+    list.id[q] = is ? key_id(key) : 0;
   }
   __syncthreads();
+  float xt = -INFINITY;
+  int idt = -1;
+  const float span = to / bins.per;
+  if (k < n) find<SW, false>(list, w, k, span, xt, idt, s);
+  if (a.top_p < 1.0) find<SW, true>(list, w, a.top_p, span, xt, idt, s);
+  // the draw: kept weights in bins of ids
+  uint64_t* ids = reinterpret_cast<uint64_t*>(s.bin);
+  const float per = static_cast<float>(BINS) / static_cast<float>(a.vocab);
+  auto place = [&](int id) { return static_cast<int>(fminf(static_cast<float>(id) * per, static_cast<float>(BINS - 1))); };
+  for (int b = tid; b < BINS; b += SN) ids[b] = 0;
+  if (tid == 0) s.n = 0;
+  __syncthreads();
+  uint64_t keep[PER];
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
-    const int i = tid * PER + q;
-    if (i >= n2) break;
-    s.key[i] = id_key[q];
-    s.w[i] = keep[q];
+    keep[q] = upto(list.x[q], list.id[q], xt, idt) ? w.kept(list.x[q]) : 0;
+    if (keep[q]) atomicAdd(reinterpret_cast<unsigned long long*>(&ids[place(list.id[q])]), static_cast<unsigned long long>(keep[q]));
   }
   __syncthreads();
-  sort_keys<SW>(s.key, n2);
-  mine = 0;
+  cross<SW>(ids, [&](uint64_t total) { return draw_target(u, total) + 1; }, s);
+  const uint64_t before = s.before, target = s.target;
 #pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    const int i = tid * PER + q;
-    v[q] = i < n2 && s.key[i] ? s.w[static_cast<uint32_t>(s.key[i])] : 0;
-    mine += v[q];
-  }
-  ahead = scan(mine, total);
-  const uint64_t goal = draw_target(u, total);
-#pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    if (ahead <= goal && goal < ahead + v[q]) a.token[r] = key_id(s.key[tid * PER + q] >> 32);
-    ahead += v[q];
+  for (int q = 0; q < PER; ++q) gather(keep[q] != 0 && place(list.id[q]) == s.at, list.x[q], list.id[q], s);
+  __syncthreads();
+  const int m = s.n;
+  for (int i = tid; i < m; i += SN) s.w[i] = w.of(key_logit(s.key[i]));
+  __syncthreads();
+  for (int i = tid; i < m; i += SN) {
+    const uint32_t key = static_cast<uint32_t>(s.key[i]);
+    uint64_t below = before;   // with the lower ids of the bin: larger low words
+    for (int j = 0; j < m; ++j)
+      if (static_cast<uint32_t>(s.key[j]) > key) below += s.w[j];
+    if (below < target && target <= below + s.w[i]) a.token[r] = key_id(s.key[i]);
   }
   __syncthreads();
   return true;
@@ -572,7 +554,7 @@ __global__ __launch_bounds__(64 * SW, SW == SW_MAX || FILTER ? 4 : 8) void k_sam
         best = fmaxf(best, x);
       });
     else {
-      row.each4([&](const float (&v)[4], int id) {
+      row.each4([&](const float (&v)[4], const auto& id) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           most[e] = fmaxf(most[e], v[e]);
@@ -637,10 +619,10 @@ __global__ __launch_bounds__(64 * SW, SW == SW_MAX || FILTER ? 4 : 8) void k_sam
       row.each([&](float x, int id) { mine += Weigh::biased(w.real(x)); });
       mine -= static_cast<uint64_t>(row.rounds) * 4 * Weigh::BIAS;
     } else {
-      row.each4([&](const float (&x)[4], int id) {
+      row.each4([&](const float (&x)[4], const auto& id) {
         bool in[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) in[e] = upto(x[e], id + e, xt, idt);
+        for (int e = 0; e < 4; ++e) in[e] = upto(x[e], id[e], xt, idt);
         if (!__any(in[0] || in[1] || in[2] || in[3])) return;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {

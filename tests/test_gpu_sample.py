@@ -174,3 +174,31 @@ def test_captured_sampling_replays():
         want = sample(y, w, top_p=0.9, top_k=300)
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("n,V", [(6, 131071), (700, 6000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_hundreds_of_kept_tokens(n, V, dtype):
+    say("case: hundreds kept", n, V, dtype)
+    x, u = rows(n, V, 11, dtype)
+    for k in (129, 500, 1000):
+        check(x, u, top_k=k)
+        check(x, u, top_k=k, top_p=0.97, temperature=2.0)
+        check(x, u, top_k=k, top_p=0.9, min_p=0.01, temperature=2.0)
+
+
+@pytest.mark.parametrize("n", [4, 600])
+def test_kept_tokens_that_lie_or_weigh_alike(n):
+    # ids next to each other in a large vocabulary, equal logits, two levels
+    say("case: alike", n)
+    V = 1 << 17
+    x, u = torch.full((n, V), -30.0, device="cuda"), torch.rand(n, generator=torch.Generator().manual_seed(12)).cuda()
+    g = torch.Generator("cuda").manual_seed(13)
+    x[:, 70000:70900] = torch.randn(n, 900, device="cuda", generator=g)
+    x[::2, 70000:70900] = x[::2, 70000:70900].round()
+    check(x, u, top_k=700)
+    check(x, u, top_k=600, top_p=0.8)
+    x[:, 70000:70900] = 1.0
+    check(x, u, top_k=800, top_p=0.5)
+    x[:, 100:400] = 1.5
+    check(x, u, top_k=500, top_p=0.9)
