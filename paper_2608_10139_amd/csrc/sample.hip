@@ -2,9 +2,17 @@
 // AI_TRANSFORM): temperature, top-k, top-p, min-p, inverse distribution in the
 // order of ids.
 //
-// A workgroup of 16 waves per row, each wave a run of ids; every pass reads the row again,
+// A workgroup of 16 or 4 waves per row, each wave a run of ids; every pass reads the row again,
 // from the L2 (held in registers, 32 logits per thread, it left none for the passes
 // to overlap: 580 us for 4,096 rows of 32,000 against 465).
+//
+// Bound: the vector unit, fp64 first of all (a weight is about 20 fp64 instructions), on the CUs that
+// have a row; one row after its latencies, a pass per 2 us or so.  Rows of 32,000 fp32 logits, us:
+//             temperature 0  no filter  top-k 50  top-k 1,000  top-p 0.9
+//   1 row            7          15         19          28          40
+//   256 rows         9          20         22          31          47
+//   2,048 rows      25         125         89         225         279   (262 MB: 55 us for one reading)
+// and 96 rows of 131,071 bf16 logits with top-k 1,000 and top-p 0.95 60, on 96 of the 256 CUs.
 //
 // Weights are whole numbers, round(2^S exp((x - m) / T)) from fp64 exponentials
 // (below), S such that a whole vocabulary's sum fits 62 bits: sums do not
@@ -18,6 +26,7 @@
 // the same way, by counts or by weights: a histogram over the distance to the
 // maximum (2,048 bins in LDS), the bin in which the count or the sum reaches its
 // target, and in that bin the token itself, by comparing its tokens (60 or so) with each other.
+// Where top-k leaves few tokens (draw_few) the steps after it are taken among those alone.
 // A bin with more than CAP tokens (equal logits, a far outlier) is halved bit by bit instead.
 #include "aiq_internal.h"
 #include "dev_util.h"
@@ -446,7 +455,7 @@ __device__ __forceinline__ bool draw_few(const R& row, const Weigh& w, const flo
   const int n = s.n;
   if (n > CAP) return false;
   const int k = a.top_k < n ? a.top_k : n;
-  if (n <= 128) {   // by comparing all with all, SN / 128 threads or more per token: no sort's chain of steps
+  if (n <= 128) {   // by comparing all with all, SN / 128 threads or more per token: fewer barriers
     const int each = SN / (n <= 64 ? 64 : 128), i = tid / each;
     for (int j = tid; j < n; j += SN) s.w[j] = w.of(key_logit(s.key[j]));
     __syncthreads();
@@ -679,7 +688,10 @@ hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
   // 16 waves per row up to the rows that leave CUs without one of theirs, 4 beyond.  Rows of 32,000 logits, 16 waves
   // against 4: without filters 512 rows 39 us against 48, 700 rows 52 against 58, 1,023 rows 68 against 71; top-p 512 rows
   // 91 against 106, 640 rows 129 against 129, 1,023 rows 177 against 155; top-k 512 rows 41 against 36, 640 58 against 38.
-  const bool wide = a.n_rows < (!filter ? 1024 : a.top_k > 0 ? 512 : 640);
+  // Also where only 16 waves gather the top-k (draw_few's bound lets in up to twice as many): 2,048 rows with top-k 700
+  // 218 us against 303, with 500 212 against 121.
+  const bool wide = a.n_rows < (!filter ? 1024 : a.top_k > 0 ? 512 : 640) ||
+                    (a.top_k > cap(4) / 2 && a.top_k <= cap(SW_MAX) / 2);
 #define AIQ_SAMPLE_K(DT_, SW_, F_) hipLaunchKernelGGL((k_sample<DT_, SW_, F_>), grid, dim3(64 * SW_), 0, s, a)
 #define AIQ_SAMPLE(DT_)                                        \
   if (wide && filter) AIQ_SAMPLE_K(DT_, SW_MAX, true);         \
