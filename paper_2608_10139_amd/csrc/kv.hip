@@ -16,6 +16,8 @@
 #include "aiq_internal.h"
 #include "dev_util.h"
 
+#include <type_traits>
+
 namespace aiq {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -42,11 +44,33 @@ __device__ __forceinline__ void kv_flag(const KvBatch& b) {
   if (b.status) atomicOr(reinterpret_cast<unsigned long long*>(b.status), static_cast<unsigned long long>(AIQ_DEV_KV_RANGE));
 }
 
-// Sequence i, or false where it is left out (its numbers do not fit, flagged; or it has no rows in this call).
-__device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, int i, KvSeq& s) {
-  s.len = uniform(b.len[i]) + b.len_add;
+// A sequence's numbers as they are in memory: read where they are used, or all at once.
+struct KvAt {
+  const KvBatch& b;
+  int i;
+  __device__ __forceinline__ int len() const { return b.len[i]; }
+  __device__ __forceinline__ int c0() const { return b.cu[i]; }
+  __device__ __forceinline__ int c1() const { return b.cu[i + 1]; }
+  __device__ __forceinline__ int e0() const { return b.blk_start[i]; }
+  __device__ __forceinline__ int e1() const { return b.blk_start[i + 1]; }
+  __device__ __forceinline__ int tail() const { return b.tail_ids ? b.tail_ids[i] : i; }
+};
+struct KvRaw {   // of a batch with cu
+  int v[6];
+  __device__ __forceinline__ int len() const { return v[0]; }
+  __device__ __forceinline__ int c0() const { return v[1]; }
+  __device__ __forceinline__ int c1() const { return v[2]; }
+  __device__ __forceinline__ int e0() const { return v[3]; }
+  __device__ __forceinline__ int e1() const { return v[4]; }
+  __device__ __forceinline__ int tail() const { return v[5]; }
+};
+// The sequence (i where there is no cu), or false where it is left out (its numbers do not fit, flagged; or it has no
+// rows in this call).
+template <typename S>
+__device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, const S& r, int i, KvSeq& s) {
+  s.len = uniform(r.len()) + b.len_add;
   if (b.cu) {
-    const int c0 = uniform(b.cu[i]), c1 = uniform(b.cu[i + 1]);
+    const int c0 = uniform(r.c0()), c1 = uniform(r.c1());
     s.row0 = c0;
     s.n = c1 - c0 + b.n_pre;
     if (c0 < 0 || c1 < c0 || c1 > b.n_rows) {
@@ -58,9 +82,9 @@ __device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, int i
     s.n = s.len == 0 ? 0 : 1;
   }
   if (s.n == 0) return false;
-  const int64_t e0 = uniform(b.blk_start[i]), e1 = uniform(b.blk_start[i + 1]);
+  const int64_t e0 = uniform(r.e0()), e1 = uniform(r.e1());
   s.bs = static_cast<int>(e0);
-  s.tail = b.tail_ids ? uniform(b.tail_ids[i]) : i;
+  s.tail = uniform(r.tail());
   const bool uses_tail = s.len % KVB != 0 || (s.len - s.n) % KVB != 0;
   if (s.len < s.n || s.len > b.max_len || e0 < 0 || (c.n_blocks == 0 && s.len >= KVB) || (e1 - e0) * KVB < s.len ||
       (uses_tail && (s.tail < 0 || s.tail >= c.n_tails))) {
@@ -184,7 +208,7 @@ __device__ __forceinline__ bool move_unit(const KvCache& c, const KvBatch& b, in
     if (d < 0) return false;   // rows before the first sequence's
     jj = static_cast<int>(d);
   }
-  return kv_seq(c, b, i, s);
+  return kv_seq(c, b, KvAt{b, i}, i, s);
 }
 
 template <int HD>
@@ -650,29 +674,33 @@ struct KvTile {
   int pos0;          // position of the tile's first query
 };
 
-// Tile u (of R rows) of the batch, or false
-template <int R>
-__device__ __forceinline__ bool kv_tile(const KvAttendArgs& a, int n, int rep, int64_t u, int h, KvTile& t) {
-  int i;
-  int64_t k;
-  if (a.b.cu) {
-    i = unit_seq(a.b, n, u, rep, R, 1);
-    k = u - unit_first(a.b, i, rep, R, 1);
+// Tile u (of R rows) of the batch, or of the sequence whose numbers are given; or false
+template <int R, typename S = int>
+__device__ __forceinline__ bool kv_tile(const KvAttendArgs& a, int n, int rep, int64_t u, KvTile& t, const S* seq = nullptr) {
+  int i = 0;
+  int64_t k = u;
+  if constexpr (!std::is_same_v<S, int>) {
+    if (!kv_seq(a.c, a.b, *seq, 0, t.s)) return false;
   } else {
-    const int tiles = (rep + 15) / 16;
-    i = static_cast<int>(u / tiles);
-    k = u - static_cast<int64_t>(i) * tiles;
-  }
-  if (!kv_seq(a.c, a.b, i, t.s)) {
-    if (!a.b.cu && t.s.len == 0) {   // an empty slot's row
-      t.r0 = static_cast<int>(k) * 16;
-      t.rows = rep - t.r0 < 16 ? rep - t.r0 : 16;
-      t.nb = 0;
-      t.pos0 = 0;
-      t.s.n = 1;
-      return true;
+    if (a.b.cu) {
+      i = unit_seq(a.b, n, u, rep, R, 1);
+      k = u - unit_first(a.b, i, rep, R, 1);
+    } else {
+      const int tiles = (rep + 15) / 16;
+      i = static_cast<int>(u / tiles);
+      k = u - static_cast<int64_t>(i) * tiles;
     }
-    return false;
+    if (!kv_seq(a.c, a.b, KvAt{a.b, i}, i, t.s)) {
+      if (!a.b.cu && t.s.len == 0) {   // an empty slot's row
+        t.r0 = static_cast<int>(k) * 16;
+        t.rows = rep - t.r0 < 16 ? rep - t.r0 : 16;
+        t.nb = 0;
+        t.pos0 = 0;
+        t.s.n = 1;
+        return true;
+      }
+      return false;
+    }
   }
   const int64_t all = static_cast<int64_t>(t.s.n) * rep;
   if (k < 0 || k * R >= all) return false;   // (k < 0: rows before the first sequence's)
@@ -910,7 +938,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
     const int64_t u = unit / c.n_kv;
     const int h = static_cast<int>(unit - u * c.n_kv);
     KvTile t;
-    if (!kv_tile<16>(a, n, rep, u, h, t)) continue;
+    if (!kv_tile<16>(a, n, rep, u, t)) continue;
     const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
     if (SPLIT && seg0 >= segs) continue;
     const int seg_end = SPLIT || segs == 0 ? seg0 + 1 : segs;
@@ -1058,7 +1086,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
   const int64_t tiles = a.b.cu ? unit_first(a.b, n, rep, 16, 1) : static_cast<int64_t>(n) * ((rep + 15) / 16);
   if (u >= tiles || u >= n_tiles) return;
   KvTile t;
-  if (!kv_tile<16>(a, n, rep, u, h, t)) return;
+  if (!kv_tile<16>(a, n, rep, u, t)) return;
   const int segs = (t.nb + KV_SEG - 1) / KV_SEG;
   const int64_t step = static_cast<int64_t>(slot_rows) * (HD + 2);
   const float* slot = a.part + unit * n_seg * step;
@@ -1128,17 +1156,79 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
 
 // ------------------------------------------------------------------ several rows per sequence
 // A workgroup of four waves per 128 query rows of a (sequence, K/V head), 32 rows
-// (two lane-column tiles) per wave, all waves walking the same blocks: a block's bytes
+// (two lane-column tiles) per wave, all waves walking the same blocks, two at a step: a block's bytes
 // become fp16 fragments once per workgroup, in LDS, in the order in which the products
-// take them (every access 16 bytes per lane, in lane order), the next block's bytes in
+// take them (every access 16 bytes per lane, in lane order), the next two steps' bytes in
 // flight meanwhile.  Bound: the softmax's VALU work (16 scores per lane and block of
-// 32 keys, 8 exponentials of 4 issue slots each per tile) beside 32 matrix instructions.
+// 32 keys, 8 exponentials of 4 issue slots each per tile) beside 32 matrix instructions, and the tail of the last
+// tiles.  64 sequences of about 900 tokens with 128 new ones, 24/8 heads of 128: 160 us, 650
+// TFLOP/s of products that are seen; 16 sequences of 4,000 with 512 830 TFLOP/s.
 constexpr int KV_ROWS = 128;
 constexpr int KV_LIST = 64;      // numbers and scales of twice as many blocks are in LDS
 constexpr int KV_AHEAD = 4;      // blocks whose bytes are in flight or staged
 
-template <int HD, bool BF>
-__global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64_t n_tiles) {
+// The tiles of a batch of up to 256 sequences in the order of descending lengths, so that long ones do not start last:
+// lengths by class, sixteen to an octave below max_len, sequences of a class in their own order.
+struct KvOrder {
+  int tiles[128];            // of the classes
+  int sum[4], first;
+  KvRaw seq;
+};
+// a value's sum over the lanes up to each (row_shr 1, 2, 4, 8, row_bcast 15, 31)
+__device__ __forceinline__ int lanes_upto(int v) {
+#define AIQ_STEP(CTRL_, ROWS_) v += __builtin_amdgcn_update_dpp(0, v, CTRL_, ROWS_, 0xF, false)
+  AIQ_STEP(0x111, 0xF);
+  AIQ_STEP(0x112, 0xF);
+  AIQ_STEP(0x114, 0xF);
+  AIQ_STEP(0x118, 0xF);
+  AIQ_STEP(0x142, 0xA);
+  AIQ_STEP(0x143, 0xC);
+#undef AIQ_STEP
+  return v;
+}
+// Tile u: its sequence and the first tile of that; false: past the last.  All threads together.
+__device__ __forceinline__ bool kv_order(const KvAttendArgs& a, int n, int rep, int R, int64_t u, KvOrder& s, KvRaw& seq, int& first) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  KvRaw raw;   // this thread's sequence, its tiles, its class
+  int tiles = 0, cls = 127;
+  if (tid < n) {
+    const KvAt q{a.b, tid};
+    raw = {{q.len(), q.c0(), q.c1(), q.e0(), q.e1(), q.tail()}};
+  }
+  if (tid < 128) s.tiles[tid] = 0;
+  if (tid < n) {
+    const int64_t rows = static_cast<int64_t>(raw.c1()) - raw.c0();
+    tiles = rows < 0 || rows > a.b.n_rows ? 1 : static_cast<int>((rows * rep + R - 1) / R);   // (1: to be flagged)
+    auto log16 = [](int x) { return static_cast<int>(__float_as_uint(static_cast<float>(x < 1 ? 1 : x)) >> 19); };
+    const int below = log16(a.b.max_len) - log16(raw.len());
+    cls = below < 0 ? 0 : below > 127 ? 127 : below;
+  }
+  __syncthreads();
+  if (tiles > 0) atomicAdd(&s.tiles[cls], tiles);
+  __syncthreads();
+  const int t0 = s.tiles[2 * lane], t1 = s.tiles[2 * lane + 1], upto = lanes_upto(t0 + t1), before = upto - t0 - t1;
+  const uint64_t hit = __ballot(before <= u && u < upto);
+  if (!hit) return false;
+  const int at = __builtin_ctzll(hit);
+  const int b0 = __builtin_amdgcn_readlane(before, at), f0 = __builtin_amdgcn_readlane(t0, at);
+  const bool second = u - b0 >= f0;
+  const int c = 2 * at + second, mine = cls == c ? tiles : 0, in = lanes_upto(mine);
+  if (lane == 63) s.sum[w] = in;
+  __syncthreads();
+  int from = b0 + (second ? f0 : 0) + in - mine;
+  for (int x = 0; x < w; ++x) from += s.sum[x];
+  if (mine > 0 && from <= u && u < from + mine) {
+    s.seq = raw;
+    s.first = from;
+  }
+  __syncthreads();
+  seq = s.seq;
+  first = uniform(s.first);
+  return true;
+}
+
+template <int HD, bool BF, bool ORDER>
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_kv_attend_rows(KvAttendArgs a, int64_t n_tiles) {
   constexpr int KC = HD / 64, NO = HD / 16, FR = 2 * KC;   // FR fragments of 16 bytes per lane of keys, and of values
   constexpr int PER = 2 * FR * 64 / 256;                   // of them per thread
   // [buffer][block][keys, values][fragment][half][lane] of 8 fp16 (the tail of a bf16 cache: bf16)
@@ -1152,13 +1242,23 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rep = a.n_heads / c.n_kv;
-  const int64_t tiles = unit_first(a.b, n, rep, KV_ROWS, 1);
-  const int64_t items = (tiles < n_tiles ? tiles : n_tiles) * c.n_kv;
+  __shared__ std::conditional_t<ORDER, KvOrder, int> ord;
+  int64_t items = n_tiles * c.n_kv;
+  if constexpr (!ORDER) {
+    const int64_t tiles = unit_first(a.b, n, rep, KV_ROWS, 1);
+    if (tiles < n_tiles) items = tiles * c.n_kv;
+  }
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t u = item / c.n_kv;
     const int h = static_cast<int>(item - u * c.n_kv);
     KvTile t;
-    if (!kv_tile<KV_ROWS>(a, n, rep, u, h, t)) continue;
+    if constexpr (ORDER) {
+      KvRaw raw;
+      int first;
+      if (!kv_order(a, n, rep, KV_ROWS, u, ord, raw, first) || !kv_tile<KV_ROWS>(a, n, rep, u - first, t, &raw)) return;
+    } else if (!kv_tile<KV_ROWS>(a, n, rep, u, t)) {
+      continue;
+    }
     const int base = t.s.len - t.s.n;
     // queries of tile x: row w * 32 + x * 16 + c16
     const uint16_t* qp[2];
@@ -1184,7 +1284,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
     const int wr = w * 32 < t.rows ? w * 32 : t.rows - 1, we = w * 32 + 31 < t.rows ? w * 32 + 31 : t.rows - 1;
     const int first = base + (t.r0 + wr) / rep, last = w * 32 < t.rows ? base + (t.r0 + we) / rep : -1;
     const int full = t.s.len / KVB < t.nb ? t.s.len / KVB : t.nb;   // the tile's blocks that are not the tail
-    uint4 raw[KV_AHEAD][PER];   // the next blocks' bytes
+    uint4 even[2][PER], odd[2][PER];   // bytes of the blocks of even pairs, of odd ones
     auto list = [&](int j0) {   // blocks j0 .. j0 + KV_LIST - 1, in the half of the list whose blocks are long past
       if (tid < KV_LIST) {
         const int to = (j0 + tid) % (2 * KV_LIST), id = j0 + tid < full ? kv_block(c, a.b, t.s.bs + j0 + tid) : -1;
@@ -1214,23 +1314,20 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
     };
     list(0);
 #pragma unroll
-    for (int d = 0; d < KV_AHEAD; ++d) {
+    for (int d = 0; d < 2; ++d) {
 #pragma unroll
-      for (int x = 0; x < PER; ++x) raw[d][x] = make_uint4(0, 0, 0, 0);   // (a pair's second block where there is none: weighs nothing)
-      load(raw[d], d);
+      for (int x = 0; x < PER; ++x) even[d][x] = odd[d][x] = make_uint4(0, 0, 0, 0);   // (a pair's second block where there is none: weighs nothing)
+      load(even[d], d);
+      load(odd[d], 2 + d);
     }
-    stage(raw[0], 0, 0);
-    stage(raw[1], 0, 1);
-    for (int j = 0; j < full; j += 2) {   // blocks j and j + 1
-      const int buf = (j >> 1) & 1;
+    stage(even[0], 0, 0);
+    stage(even[1], 0, 1);
+    // blocks j and j + 1, staged in buf; the next pair's bytes are in `next`, those of the pair after it go into `then`
+    auto step = [&](int j, int buf, const uint4 (&next)[2][PER], uint4 (&then)[2][PER]) {
       const KvScale sc[2] = {scales[j % (2 * KV_LIST)], scales[(j + 1) % (2 * KV_LIST)]};
-#pragma unroll
-      for (int d = 0; d + 2 < KV_AHEAD; ++d)
-#pragma unroll
-        for (int x = 0; x < PER; ++x) raw[d][x] = raw[d + 2][x];
       if ((j + KV_AHEAD) % KV_LIST == 0) list(j + KV_AHEAD);
-      load(raw[KV_AHEAD - 2], j + KV_AHEAD);
-      load(raw[KV_AHEAD - 1], j + KV_AHEAD + 1);
+      load(then[0], j + KV_AHEAD);
+      load(then[1], j + KV_AHEAD + 1);
       __syncthreads();   // blocks j, j + 1 staged; the other buffer's consumed
       const int tok0 = j * KVB;
       if (tok0 <= last) {
@@ -1279,9 +1376,13 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
             }
       }
       if (j + 2 < full) {
-        stage(raw[0], buf ^ 1, 0);
-        stage(raw[1], buf ^ 1, 1);
+        stage(next[0], buf ^ 1, 0);
+        stage(next[1], buf ^ 1, 1);
       }
+    };
+    for (int j = 0; j < full; j += 4) {
+      step(j, 0, odd, even);
+      if (j + 2 < full) step(j + 2, 1, even, odd);
     }
     if (full < t.nb) {   // the tail: its rows as fragments of their own type
       const int tok0 = full * KVB, left = t.s.len - tok0;
@@ -1378,6 +1479,7 @@ __global__ __launch_bounds__(256, 2) void k_kv_attend_rows(KvAttendArgs a, int64
         }
       }
     }
+    if (ORDER) return;   // (a workgroup per item)
     __syncthreads();
   }
 }
@@ -1397,11 +1499,12 @@ static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
   s.rows = b.cu || rep > 16 ? 16 : rep;
   const int64_t big = b.cu ? b.n_rows * rep / KV_ROWS + b.n_seq : 0;
   // Tiles of KV_ROWS rows against tiles of 16, 24/8 heads of 128 and 32/8 heads of 64: 256 sequences of about 300 tokens
-  // with 8 new rows each 89 us against 67 and 49 against 38, with 16 (48 and 64 rows per K/V head) 102 against 115
-  // and 57 against 58, with 32 110 against 174 and 95 against 96; 64 sequences of 900 with 16 71 against 98 and 35
-  // against 52.  Few tiles leave CUs without one: 16 sequences of 2,000 with 16 (176 workgroups) 63 against 46, 4 of
-  // 4,000 with 64 (80) 117 against 81, 16 with 64 (320) 86 against 139.
-  s.many = b.cu && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY && big * c.n_kv >= 256;
+  // with 8 new rows each 81 us against 71 and 45 against 38, with 16 (48 and 64 rows per K/V head) 90 against 124
+  // and 54 against 58, with 32 101 against 191 and 58 against 97; 64 sequences of 900 with 16 48 against 95 and 35
+  // against 56.  Where the tiles of 16 are few they run at once, four waves to a tile's keys: 16 sequences of 2,000 with
+  // 16 (512 and 640 of them) 65 against 47 and 48 against 37, with 32 (896, 1,152) 67 against 81 and 52 against 57; 4 of
+  // 4,000 with 64 (416, 544) 116 against 83 and 84 against 64, with 128 (800, 1,056) 121 against 137 and 87 against 93.
+  s.many = b.cu && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY && s.tiles * c.n_kv >= 768;
   if (s.many) {
     s.tiles = big;
     return s;
@@ -1437,11 +1540,23 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t s) {
   const bool bf = a.c.act == ACT_BF16;
   if (k.many) {
     const dim3 grid(static_cast<unsigned>(items < (1 << 20) ? items : 1 << 20));
-#define AIQ_KV_ROWS(HD_, BF_) hipLaunchKernelGGL((k_kv_attend_rows<HD_, BF_>), grid, dim3(256), 0, s, a, k.tiles)
-    if (a.c.hd == 64 && bf) AIQ_KV_ROWS(64, true);
-    else if (a.c.hd == 64) AIQ_KV_ROWS(64, false);
-    else if (bf) AIQ_KV_ROWS(128, true);
-    else AIQ_KV_ROWS(128, false);
+    // In the order of lengths, without empty tiles, against the order of the batch (a tile more per sequence than its rows
+    // may need), 24/8 heads of 128 and 32/8 heads of 64: 64 sequences of about 900 tokens (sigma 0.4) with 128 new rows
+    // 160 us against 220 and 118 against 139; 256 of 300 with 32 116 against 143 and 61 against 119; 256 of 40 with
+    // 256 411 against 402 and 314 against 298.
+    const bool order = a.b.n_seq <= 256 && items <= 1 << 20;   // (a thread per sequence, a workgroup per tile)
+#define AIQ_KV_ROWS(HD_, BF_)                                                                            \
+  if (order) hipLaunchKernelGGL((k_kv_attend_rows<HD_, BF_, true>), grid, dim3(256), 0, s, a, k.tiles);  \
+  else hipLaunchKernelGGL((k_kv_attend_rows<HD_, BF_, false>), grid, dim3(256), 0, s, a, k.tiles)
+    if (a.c.hd == 64 && bf) {
+      AIQ_KV_ROWS(64, true);
+    } else if (a.c.hd == 64) {
+      AIQ_KV_ROWS(64, false);
+    } else if (bf) {
+      AIQ_KV_ROWS(128, true);
+    } else {
+      AIQ_KV_ROWS(128, false);
+    }
 #undef AIQ_KV_ROWS
     return hipGetLastError();
   }

@@ -497,3 +497,28 @@ def test_two_streams_and_two_graphs_at_once():
         eager = calls[0][0].attend(*calls[0][1:])
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, want)) and torch.equal(eager, want[0])
+
+
+@pytest.mark.parametrize("n", [70, 300])
+def test_many_rows_of_sequences_of_many_lengths(n):
+    # lengths far apart, sequences without rows between; then one whose numbers do not fit
+    say("many lengths", n)
+    r = np.random.default_rng(51)
+    lens = np.minimum(np.exp(r.normal(5.0, 0.9, n)).astype(np.int64) + 1, 3000)
+    new = np.where(r.random(n) < 0.2, 0, np.minimum(lens, r.integers(60, 200, n)))
+    c = Case(lens, 8, 4, 64, torch.float16, 52)
+    c.write(lens, lens)
+    q = c.rows("q", lens, new)
+    out = c.cache.attend(c.batch(lens, new), q)
+    c.check_attend(lens, new, out)
+    bad = int(np.flatnonzero(new)[3])
+    over = lens.copy()
+    over[bad] = 4000
+    at = starts(new)
+    b = c.cache.batch(i32(over), c.blk_start, 3000, cu=i32(at), blk_ids=c.blk_ids, tail_ids=c.tail_ids)
+    again = c.cache.attend(b, q)
+    assert int(c.cache.status.item()) == B.AIQ_DEV_KV_RANGE
+    keep = np.ones(int(at[-1]), bool)
+    keep[at[bad]:at[bad + 1]] = False
+    keep = torch.from_numpy(keep).cuda()
+    assert torch.equal(again[keep], out[keep])
