@@ -1,4 +1,4 @@
-// AI_TRANSFORM: greedy generation after the prefill (Table 1 maps it to a
+// AI_TRANSFORM: generation after the prefill (Table 1 maps it to a
 // causal-LM forward with generative decoding, output masked with a pad id;
 // Section 4, Q3 and Q5), and the LIKE match over the generated tokens.
 //
@@ -6,10 +6,12 @@
 // projections as the prefill (M = number of sequences), a decode attention
 // kernel over the sequence's kept keys and values, and the full-vocabulary
 // head as a GEMM whose epilogue keeps only each row's maximum per 64 columns,
-// followed by a row argmax over those.  Keys and values
+// followed by a row argmax over those; or the head's logits and a draw from
+// them (sample.hip).  Keys and values
 // of the prompt stay where the prefill put them (the chunk's per-layer q|k|v
 // rows, plus the shared prefix's rows); those of generated tokens go to a
-// per-layer cache [sequence][step][2 d_kv].  Everything runs on the launch
+// per-layer cache [sequence][step][2 d_kv]; or both go to an 8-bit cache
+// (kv.hip).  Everything runs on the launch
 // stream; counts come from device memory.
 #include "aiq_internal.h"
 #include "dev_util.h"

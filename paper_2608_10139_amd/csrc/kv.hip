@@ -137,7 +137,9 @@ __device__ __forceinline__ int unit_seq(const KvBatch& b, int n, int64_t u, int 
 // ------------------------------------------------------------------ write and read
 // A wave per (32-token block of a sequence that the call touches, K/V head);
 // heads of a block are neighbours, so rows are read whole between them.
-// Bound: HBM (2 bytes per element in, 1 out for full blocks; 2 out for the tail).
+// Bound: HBM (2 bytes per element in, 1 out for full blocks; 2 out for the tail).  24/8 heads of 128: 1,500 prompts
+// of about 120 tokens written in 332 us (1.35 GB, 4.1 TB/s) and read back in 262 (1.34 GB, 5.1 TB/s; a copy
+// reaches 4.8); 2,000 whole sequences read in 61.
 // The wave of a sequence's first touched block reads what the tail holds of
 // it, and then writes the new tail: no other wave touches the tail.
 
@@ -211,13 +213,96 @@ __device__ __forceinline__ bool move_unit(const KvCache& c, const KvBatch& b, in
   return kv_seq(c, b, KvAt{b, i}, i, s);
 }
 
+// Block `id` of head h from its 32 tokens, the first one at position p0: those below `before` from the tail (tk, tv),
+// the others from the rows that row_k and row_v give.
+template <int HD, typename K, typename V>
+__device__ __forceinline__ void write_block(const KvCache& c, int id, int h, int p0, int before, const uint16_t* tk, const uint16_t* tv,
+                                            K row_k, V row_v) {
+  constexpr int KC = HD / 64;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+  const int64_t at = static_cast<int64_t>(id) * c.n_kv + h;
+  uint4 kr[2 * KC][2];
+  uint32_t m = 0;
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) {
+    const int t = tt * 16 + c16, at_p = p0 + t;
+    const uint16_t* p = (at_p < before ? tk + t * HD : row_k(at_p)) + g * 16;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) kr[tt * KC + kc][e] = *reinterpret_cast<const uint4*>(p + kc * 64 + e * 8);
+  }
+  uint2 vr[KC][2][4];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = tt * 16 + g * 4 + r, at_p = p0 + t;
+      const uint16_t* p = (at_p < before ? tv + t * HD : row_v(at_p)) + c16 * 4;
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) vr[kc][tt][r] = *reinterpret_cast<const uint2*>(p + kc * 64);
+    }
+#pragma unroll
+  for (int i = 0; i < 2 * KC; ++i)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      m = abs_max(abs_max(abs_max(abs_max(m, kr[i][e].x), kr[i][e].y), kr[i][e].z), kr[i][e].w);
+  float inv;
+  float sc = block_scale(m, c.act, inv);
+  if (lane == 0) c.ks[at] = sc;
+  uint8_t* kb = c.k + at * (KVB * HD);
+#pragma unroll
+  for (int i = 0; i < 2 * KC; ++i) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t x[4] = {kr[i][e].x, kr[i][e].y, kr[i][e].z, kr[i][e].w};
+      uint32_t b[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z)
+        b[z] = quant(act2f(static_cast<uint16_t>(z & 1 ? x[z / 2] >> 16 : x[z / 2] & 0xFFFFu), c.act), sc, inv);
+      w[e * 2] = pack4(b[0], b[1], b[2], b[3]);
+      w[e * 2 + 1] = pack4(b[4], b[5], b[6], b[7]);
+    }
+    *reinterpret_cast<uint4*>(kb + (i * 64 + lane) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  m = 0;
+#pragma unroll
+  for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m = abs_max(abs_max(m, vr[kc][tt][r].x), vr[kc][tt][r].y);
+  sc = block_scale(m, c.act, inv);
+  if (lane == 0) c.vs[at] = sc;
+  uint8_t* vb = c.v + at * (KVB * HD);
+#pragma unroll
+  for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+      const int d = kc * 64 + c16 * 4 + z;   // its 8 tokens of this lane group
+      uint32_t w[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        uint32_t b[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t x = z < 2 ? vr[kc][tt][r].x : vr[kc][tt][r].y;
+          b[r] = quant(act2f(static_cast<uint16_t>(z & 1 ? x >> 16 : x & 0xFFFFu), c.act), sc, inv);
+        }
+        w[tt] = pack4(b[0], b[1], b[2], b[3]);
+      }
+      *reinterpret_cast<uint2*>(vb + ((d / 32) * 64 + g * 16 + d % 16) * 16 + (d % 32 / 16) * 8) =
+          make_uint2(w[0], w[1]);
+    }
+}
+
 template <int HD>
 __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
-  constexpr int KC = HD / 64;
   const KvCache& c = a.c;
   const int n = kv_count(a.b);
   if (n <= 0) return;
-  const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+  const int lane = threadIdx.x & 63;
   const int64_t units = move_count(a.b, n);
   const int64_t wave = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 6;
   const int64_t n_waves = (static_cast<int64_t>(gridDim.x) * blockDim.x) >> 6;
@@ -243,83 +328,7 @@ __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
     };
     if ((j + 1) * KVB <= s.len) {
       const int id = kv_block(c, a.b, s.bs + j);
-      if (id >= 0) {
-        const int64_t at = static_cast<int64_t>(id) * c.n_kv + h;
-        uint4 kr[2 * KC][2];
-        uint32_t m = 0;
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          const int t = tt * 16 + c16, at_p = j * KVB + t;
-          const uint16_t* p = (at_p < before ? tk + t * HD : row_k(at_p)) + g * 16;
-#pragma unroll
-          for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) kr[tt * KC + kc][e] = *reinterpret_cast<const uint4*>(p + kc * 64 + e * 8);
-        }
-        uint2 vr[KC][2][4];
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int t = tt * 16 + g * 4 + r, at_p = j * KVB + t;
-            const uint16_t* p = (at_p < before ? tv + t * HD : row_v(at_p)) + c16 * 4;
-#pragma unroll
-            for (int kc = 0; kc < KC; ++kc) vr[kc][tt][r] = *reinterpret_cast<const uint2*>(p + kc * 64);
-          }
-#pragma unroll
-        for (int i = 0; i < 2 * KC; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            m = abs_max(abs_max(abs_max(abs_max(m, kr[i][e].x), kr[i][e].y), kr[i][e].z), kr[i][e].w);
-        float inv;
-        float sc = block_scale(m, c.act, inv);
-        if (lane == 0) c.ks[at] = sc;
-        uint8_t* kb = c.k + at * (KVB * HD);
-#pragma unroll
-        for (int i = 0; i < 2 * KC; ++i) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const uint32_t x[4] = {kr[i][e].x, kr[i][e].y, kr[i][e].z, kr[i][e].w};
-            uint32_t b[8];
-#pragma unroll
-            for (int z = 0; z < 8; ++z)
-              b[z] = quant(act2f(static_cast<uint16_t>(z & 1 ? x[z / 2] >> 16 : x[z / 2] & 0xFFFFu), c.act), sc, inv);
-            w[e * 2] = pack4(b[0], b[1], b[2], b[3]);
-            w[e * 2 + 1] = pack4(b[4], b[5], b[6], b[7]);
-          }
-          *reinterpret_cast<uint4*>(kb + (i * 64 + lane) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        m = 0;
-#pragma unroll
-        for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) m = abs_max(abs_max(m, vr[kc][tt][r].x), vr[kc][tt][r].y);
-        sc = block_scale(m, c.act, inv);
-        if (lane == 0) c.vs[at] = sc;
-        uint8_t* vb = c.v + at * (KVB * HD);
-#pragma unroll
-        for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-          for (int z = 0; z < 4; ++z) {
-            const int d = kc * 64 + c16 * 4 + z;   // its 8 tokens of this lane group
-            uint32_t w[2];
-#pragma unroll
-            for (int tt = 0; tt < 2; ++tt) {
-              uint32_t b[4];
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const uint32_t x = z < 2 ? vr[kc][tt][r].x : vr[kc][tt][r].y;
-                b[r] = quant(act2f(static_cast<uint16_t>(z & 1 ? x >> 16 : x & 0xFFFFu), c.act), sc, inv);
-              }
-              w[tt] = pack4(b[0], b[1], b[2], b[3]);
-            }
-            *reinterpret_cast<uint2*>(vb + ((d / 32) * 64 + g * 16 + d % 16) * 16 + (d % 32 / 16) * 8) =
-                make_uint2(w[0], w[1]);
-          }
-      }
+      if (id >= 0) write_block<HD>(c, id, h, j * KVB, before, tk, tv, row_k, row_v);
     }
     if (jj != 0 || s.len % KVB == 0) continue;
     // the tail: the new tokens of the last block, after this wave's own reads of the old one
@@ -330,6 +339,59 @@ __global__ __launch_bounds__(256) void k_kv_write(KvMoveArgs a) {
       *reinterpret_cast<uint4*>(tk + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(row_k(t) + e);
       *reinterpret_cast<uint4*>(tv + t % KVB * HD + e) = *reinterpret_cast<const uint4*>(row_v(t) + e);
     }
+  }
+}
+
+// One row per sequence (no cu): a wave per sequence writes its row of all heads into the tail; the blocks that a
+// workgroup's sequences complete, one in 32 steps, are then its eight waves', a head each at a time (4 us for one: cold
+// loads, then the rounding).  A workgroup takes up to eight sequences, fewer where that leaves CUs without any: 64
+// that complete a block at once 55 us by eights, 13 by ones.  2,000 sequences of 24/8 heads of 128, a 32nd of them with a
+// block complete, 20 us where a wave per (sequence, head) took 23; a query of 16,384 rows with 128 steps of 4 layers
+// 720 ms for 753.
+template <int HD>
+__global__ __launch_bounds__(512) void k_kv_write_one(KvMoveArgs a, int per) {
+  __shared__ int full[8][3];   // of the sequences that complete a block: its number, its first token, the tail
+  const KvCache& c = a.c;
+  const int n = kv_count(a.b);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int i0 = blockIdx.x * per; i0 < n; i0 += gridDim.x * per) {
+    KvSeq s;
+    const bool is = w < per && i0 + w < n && kv_seq(c, a.b, KvAt{a.b, i0 + w}, i0 + w, s);
+    const int id = is && s.len % KVB == 0 ? kv_block(c, a.b, s.bs + s.len / KVB - 1) : -1;
+    if (lane == 0) {
+      full[w][0] = id;
+      full[w][1] = id < 0 ? 0 : s.len - KVB;
+      full[w][2] = id < 0 ? 0 : s.tail;
+    }
+    if (is && s.len % KVB != 0) {
+      const int t = s.len % KVB - 1, pieces = c.n_kv * (HD / 8);
+      const uint16_t* k = a.r.k + s.row0 * a.r.k_ld;
+      const uint16_t* v = a.r.v + s.row0 * a.r.v_ld;
+      uint16_t* tk = tail_at(c, s.tail, 0, 0) + t * HD;
+      uint16_t* tv = tail_at(c, s.tail, 1, 0) + t * HD;
+      auto to = [](int x) { return x / (HD / 8) * static_cast<int64_t>(KVB * HD) + x % (HD / 8) * 8; };
+      for (int x = lane; x < pieces; x += 128) {
+        const int y = x + 64 < pieces ? x + 64 : x;
+        const uint4 kx = *reinterpret_cast<const uint4*>(k + x * 8), vx = *reinterpret_cast<const uint4*>(v + x * 8);
+        const uint4 ky = *reinterpret_cast<const uint4*>(k + y * 8), vy = *reinterpret_cast<const uint4*>(v + y * 8);
+        *reinterpret_cast<uint4*>(tk + to(x)) = kx;
+        *reinterpret_cast<uint4*>(tv + to(x)) = vx;
+        *reinterpret_cast<uint4*>(tk + to(y)) = ky;
+        *reinterpret_cast<uint4*>(tv + to(y)) = vy;
+      }
+    }
+    __syncthreads();
+    for (int q = 0; q < per; ++q) {
+      const int bid = uniform(full[q][0]), p0 = uniform(full[q][1]), tail = uniform(full[q][2]);
+      if (bid < 0) continue;
+      for (int h = w; h < c.n_kv; h += 8) {
+        const uint16_t* k = a.r.k + (i0 + q) * a.r.k_ld + h * HD;
+        const uint16_t* v = a.r.v + (i0 + q) * a.r.v_ld + h * HD;
+        write_block<HD>(c, bid, h, p0, p0 + KVB - 1, tail_at(c, tail, 0, h), tail_at(c, tail, 1, h), [&](int) { return k; },
+                        [&](int) { return v; });
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -446,12 +508,17 @@ hipError_t launch_kv_write(const KvCache& c, const KvBatch& b, const KvRows& r, 
   if (b.n_seq == 0 || (b.n_rows == 0 && b.n_pre == 0)) return hipSuccess;
   if (b.n_pre < 0 || (b.n_pre > 0 && (!b.cu || !r.pk || !r.pv))) return hipErrorInvalidValue;
   const KvMoveArgs a{c, b, r};
-  // (a bound from the host only: the sequences may be few)
-  const dim3 grid(kv_grid(move_units(b) * c.n_kv, b.n_ptr ? 1 << 13 : 1 << 16));
-  if (c.hd == 64)
+  // (with n_ptr a bound from the host only: the sequences may be few)
+  const int cap = b.n_ptr ? 1 << 13 : 1 << 16, per = b.n_seq < 2048 ? (b.n_seq + 255) / 256 : 8;
+  const dim3 grid(kv_grid(move_units(b) * c.n_kv, cap)), one(kv_grid((b.n_seq + per - 1) / per * static_cast<int64_t>(4), cap));
+  if (c.hd == 64 && b.cu)
     hipLaunchKernelGGL((k_kv_write<64>), grid, dim3(256), 0, s, a);
-  else if (c.hd == 128)
+  else if (c.hd == 64)
+    hipLaunchKernelGGL((k_kv_write_one<64>), one, dim3(512), 0, s, a, per);
+  else if (c.hd == 128 && b.cu)
     hipLaunchKernelGGL((k_kv_write<128>), grid, dim3(256), 0, s, a);
+  else if (c.hd == 128)
+    hipLaunchKernelGGL((k_kv_write_one<128>), one, dim3(512), 0, s, a, per);
   else
     return hipErrorInvalidValue;
   return hipGetLastError();
@@ -509,10 +576,12 @@ hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, h
 // m follows the maximum only when that is more than 8 above it (so weights
 // stay below 2^8 and, with the fixed factor 2^7, in fp16's normal range down to 2^-29 of
 // the largest).  fp16 holds the weights to 2^-12, as the 16-bit attention does.
+// Bound: HBM, as every byte of the cache is read once: 2,000 sequences of about 200 tokens (24/8 heads of 128, waves
+// alone) 224 us for 1.14 GB, 5.1 TB/s; 4 of 100,000 (32/8 heads of 64, split) 83 us for 417 MB, 5.0 TB/s; one of
+// 171 tokens 6.5 us, the chain of one wave's loads and products.
 constexpr int KV_SEG = 16;       // blocks per segment
 constexpr float KV_SLACK = 8.0f, KV_UP = 7.0f;
-constexpr int KV_MANY = 48;          // rows per sequence from which on tiles of KV_ROWS take them
-
+constexpr int KV_MANY = 48;      // rows per sequence from which on tiles of KV_ROWS take them
 
 __device__ __forceinline__ float swap_max(float v) {   // over the wave's four lane groups
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
