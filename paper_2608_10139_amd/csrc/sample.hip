@@ -3,7 +3,7 @@
 // order of ids.
 //
 // A workgroup of 16 or 4 waves per row, each wave a run of ids; every pass reads the row again,
-// from the L2 (held in registers, 32 logits per thread, it left none for the passes
+// from the L2 where that still holds it (held in registers, 32 logits per thread, it left none for the passes
 // to overlap: 580 us for 4,096 rows of 32,000 against 465).
 //
 // Bound: the vector unit, fp64 first of all (a weight is about 20 fp64 instructions), on the CUs that
@@ -11,7 +11,7 @@
 //             temperature 0  no filter  top-k 50  top-k 1,000  top-p 0.9
 //   1 row            7          15         19          28          40
 //   256 rows         9          20         22          31          47
-//   2,048 rows      25         125         89         225         279   (262 MB: 55 us for one reading)
+//   2,048 rows      25         125         89         225         279   (262 MB: 55 us a reading, of two at least)
 // and 96 rows of 131,071 bf16 logits with top-k 1,000 and top-p 0.95 60, on 96 of the 256 CUs.
 //
 // Weights are whole numbers, round(2^S exp((x - m) / T)) from fp64 exponentials
