@@ -215,3 +215,12 @@ def test_sampled_8_bit_generation_with_end_token_and_like():
     o = run(t, m, dm, base, kv_dtype="i8", sample_u=other)
     np.testing.assert_array_equal(o["gen"][::2], free["gen"][::2])
     assert np.any(o["gen"][1::2] != free["gen"][1::2])
+
+
+def test_one_generated_token_needs_no_step():
+    say("case: one token")
+    m, dm = model("hd64")
+    t = tables(50, 72)
+    a, b = (run(t, m, dm, query(1, npre=5), kv_dtype=kv) for kv in ("i8", "f16"))
+    assert a["status"] == 0 and a["n_selected"] > 0
+    np.testing.assert_array_equal(a["gen"], b["gen"])

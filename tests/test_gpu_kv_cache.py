@@ -522,3 +522,51 @@ def test_many_rows_of_sequences_of_many_lengths(n):
     keep[at[bad]:at[bad + 1]] = False
     keep = torch.from_numpy(keep).cuda()
     assert torch.equal(again[keep], out[keep])
+
+
+def test_single_rows_read_back_and_sequences_without_blocks():
+    say("single rows")
+    lens = [1, 31, 32, 33, 0, 64, 300]
+    c = Case(lens, 4, 2, 64, torch.bfloat16, 61)
+    c.write(lens, lens)
+    k, v = c.cache.read(c.batch(lens, [1] * len(lens), single=True))
+    for got, what in ((k, 0), (v, 1)):
+        for i, L in enumerate(lens):
+            if L:
+                want = torch.from_numpy(c.held(i, L)[what][-1]).to(torch.float32).bfloat16()
+                assert torch.equal(got[i].cpu(), want), L
+    say("tails alone")
+    lens = np.array([1, 17, 31, 0])
+    c = Case(lens, 4, 2, 64, torch.float16, 62, paged=False)
+    c.cache = DeviceKvCache(0, 4, 2, 64, torch.float16)
+    c.write(lens, lens)
+    c.check_read(lens)
+    one = (lens > 0).astype(np.int64)
+    q = torch.zeros(4, 4, 64, dtype=torch.float16, device="cuda")
+    q[torch.from_numpy(lens > 0).cuda()] = c.rows("q", lens, one)
+    out = c.cache.attend(c.batch(lens, one, single=True), q)
+    c.check_attend(lens, np.ones(4, np.int64) * one, out[:3])
+    assert not bool(out[3].any())
+
+
+@pytest.mark.parametrize("n,hd", [(1, 64), (300, 128), (2100, 64)])
+def test_single_rows_complete_blocks_in_any_group(n, hd):
+    # steps of one row per sequence across a block's end, sequences at different places: what the calls with all rows hold
+    say("steps", n, hd)
+    r = np.random.default_rng(63)
+    lens = r.integers(28, 70, n)
+    c, d = (Case(lens + 6, 3, 3, hd, torch.float16, 64) for _ in range(2))
+    c.write(lens, lens)
+    for s in range(1, 7):
+        c.write(lens + s, np.ones(n, np.int64), single=True)
+    d.write(lens + 6, lens + 6)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        x, y = getattr(c.cache, name), getattr(d.cache, name)
+        full = torch.zeros(x.shape[0], dtype=torch.bool, device="cuda")   # (the last block, where it is not full, is not written)
+        at = (c.blk_ids.long().cpu().numpy())
+        for i in range(n):
+            full[torch.from_numpy(at[c.start[i]:c.start[i] + (lens[i] + 6) // BLOCK]).cuda()] = True
+        assert torch.equal(x[full], y[full]), name
+    for p, q in zip(c.cache.read(c.batch(lens + 6, lens + 6)), d.cache.read(d.batch(lens + 6, lens + 6))):
+        assert torch.equal(p, q)
+    c.ok()

@@ -202,3 +202,14 @@ def test_kept_tokens_that_lie_or_weigh_alike(n):
     check(x, u, top_k=800, top_p=0.5)
     x[:, 100:400] = 1.5
     check(x, u, top_k=500, top_p=0.9)
+
+
+def test_more_rows_than_workgroups():
+    say("case: 70,000 rows")
+    x, u = rows(700, 60, 14)
+    x, u = x.repeat(100, 1), torch.rand(70000, generator=torch.Generator().manual_seed(15)).cuda()
+    for kw in (dict(), dict(top_k=7), dict(top_p=0.8, min_p=0.01)):
+        got = sample(x, u, **kw)
+        want = torch.cat([sample(x[i:i + 700], u[i:i + 700], **kw) for i in range(0, 70000, 700)])
+        assert torch.equal(got, want)
+        check(x[-40:], u[-40:], **kw)
