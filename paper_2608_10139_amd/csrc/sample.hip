@@ -453,7 +453,10 @@ __device__ __forceinline__ bool draw_few(const R& row, const Weigh& w, const flo
   });
   __syncthreads();
   const int n = s.n;
-  if (n > CAP) return false;
+  if (n > CAP) {
+    __syncthreads();   // every wave has read the count that the next step clears
+    return false;
+  }
   const int k = a.top_k < n ? a.top_k : n;
   if (n <= 128) {   // by comparing all with all, SN / 128 threads or more per token: fewer barriers
     const int each = SN / (n <= 64 ? 64 : 128), i = tid / each;

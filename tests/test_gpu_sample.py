@@ -213,3 +213,30 @@ def test_more_rows_than_workgroups():
         want = torch.cat([sample(x[i:i + 700], u[i:i + 700], **kw) for i in range(0, 70000, 700)])
         assert torch.equal(got, want)
         check(x[-40:], u[-40:], **kw)
+
+
+@pytest.mark.parametrize("n,ks", [(6, (1500, 2000, 4000, 4096, 5000)), (300, (2000, 4000)), (700, (500, 2000))])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_top_k_of_more_candidates_than_are_gathered(n, ks, dtype):
+    """Thousands of tokens pass top-k's first bound: the steps start over on the whole row."""
+    say("case: top-k of thousands", n, ks, dtype)
+    x, u = rows(n, 20000, 17, dtype)
+    for k in ks:
+        check(x, u, top_k=k)
+        check(x, u, top_k=k, top_p=0.97, min_p=1e-4, temperature=2.0)
+
+
+@pytest.mark.parametrize("n", [2, 256, 1100])
+def test_border_of_thousands_of_equal_logits_in_many_rows(n):
+    """Levels of more equal logits than are gathered, on as many rows as workgroups are resident: the same tokens each time."""
+    say("case: thousands of equal logits", n)
+    g = torch.Generator().manual_seed(18)
+    x = torch.randint(-2, 2, (n, 9001), generator=g).float()
+    x[::3] = 0.5
+    x, u = x.cuda(), torch.rand(n, generator=g).cuda()
+    for k in (7, 500, 2600):
+        got = sample(x, u, top_k=k)
+        assert all(torch.equal(got, sample(x, u, top_k=k)) for _ in range(5))
+        check(x[-24:], u[-24:], top_k=k)
+        want = [reference(r, a, 1.0, k) for r, a in zip(x[:24].double().cpu().numpy(), u[:24].double().cpu().numpy())]
+        np.testing.assert_array_equal(got[:24].cpu().numpy(), want)
