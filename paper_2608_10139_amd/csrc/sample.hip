@@ -608,9 +608,11 @@ __global__ __launch_bounds__(64 * SW, SW == SW_MAX || FILTER ? 4 : 8) void k_sam
       for (int q = 0; q < 4; ++q) most[q] = most[q] == INFINITY ? 0.f : -INFINITY;
     }
     const int bits = 32 - __builtin_clz(static_cast<uint32_t>(V));
-    w.c = 1.4426950408889634 * fmin(1.0 / a.temperature, 1e300);
+    // (temperatures past 1e200 are that: finite logits are at most 2^129 apart and weigh the same all the same, and the
+    // distance d0 stays finite, so that -infinity weighs nothing)
+    w.c = 1.4426950408889634 * fmax(fmin(1.0 / a.temperature, 1e300), 1e-200);
     w.s = bits > 12 ? 62 - bits : 50;
-    w.d0 = fmax(-(w.s + 4.0) / w.c, -1e300);
+    w.d0 = -(w.s + 4.0) / w.c;
     w.least = a.min_p * static_cast<double>(1ull << w.s);
     float xt = -INFINITY;   // all but -infinity
     int idt = -1;

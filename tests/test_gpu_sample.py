@@ -240,3 +240,17 @@ def test_border_of_thousands_of_equal_logits_in_many_rows(n):
         check(x[-24:], u[-24:], top_k=k)
         want = [reference(r, a, 1.0, k) for r, a in zip(x[:24].double().cpu().numpy(), u[:24].double().cpu().numpy())]
         np.testing.assert_array_equal(got[:24].cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_temperatures_up_to_the_largest(dtype):
+    # every finite logit weighs the same; -infinity and NaN nothing, and no id is past the row's end
+    say("case: temperatures up to the largest", dtype)
+    for V in (5, 777, 3001):
+        x, u = rows(64, V, 16, dtype)
+        x[:, ::3] = float("-inf")
+        x[1::2, 1::3] = float("nan")
+        u[:4] = torch.tensor([0.0, 0.5, 0.999, 1.0 - 2.0 ** -24])
+        for T in (1e200, 1e290, 1e300, 1.7976931348623157e308):
+            for kw in (dict(), dict(top_k=300), dict(top_p=0.9), dict(min_p=0.5)):
+                check(x, u, temperature=T, **kw)
