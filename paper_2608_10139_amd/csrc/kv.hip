@@ -651,14 +651,16 @@ __device__ __forceinline__ float rows_f16(half8 (&q)[N]) {
 
 // What a block's scales make of its scores: times k, plus the log2 of the values' scale, and that
 // inverted for the sums.  A block with an infinity or NaN has scores of NaN instead (bad), so that
-// tokens that a row does not see can still be masked.
+// tokens that a row does not see can still be masked.  A values' scale below the least that is written (of a block that
+// never was) counts as that one: its tokens weigh what their scores say.
 struct KvScale {
   float k, log_v, inv_v;
   bool bad;
 };
 __device__ __forceinline__ KvScale kv_scale(float ks, float vs) {
   const bool bad = !(ks < INFINITY) || !(vs < INFINITY);
-  return {bad ? 1.f : ks, bad ? 0.f : __builtin_amdgcn_logf(vs), bad || vs == 0.f ? 1.f : 1.0f / vs, bad};
+  vs = bad ? 1.f : fmaxf(vs, 0x1p-80f / 127.0f);
+  return {bad ? 1.f : ks, __builtin_amdgcn_logf(vs), 1.0f / vs, bad};
 }
 
 // Scores of NaN for a block that holds one; -infinity for tokens (tok + 0 .. 3, tok + 16 .. 19) past pos.
@@ -725,6 +727,10 @@ __device__ __forceinline__ void kv_softmax(const f32x4 (&acc)[S][T][2], const fl
 }
 // a factor of scores: positive, so that the product with -infinity is that
 __device__ __forceinline__ float kv_factor(float fac, float ks) { return fmaxf(fac * ks, 0x1p-126f); }
+
+// 1 / sum of a row that sees nb blocks: 0 for an empty slot's, which sees none.  A sum of 0 over blocks comes of scores that
+// are all -infinity (an infinite query): infinity, and not a number times the numerator of 0, as the formula has it.
+__device__ __forceinline__ float kv_inverse(float l, int nb) { return nb == 0 ? 0.f : 1.0f / l; }
 
 // softmax state of one row: reference, sum, one value of the numerator
 __device__ __forceinline__ void kv_fold(float& m, float& l, float& o, float mp, float lp, float op) {
@@ -1062,7 +1068,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
       }
       if (c16 < t.rows) {
         const int q = t.r0 + c16;
-        const float inv = x.l[0] == 0.f ? 0.f : 1.0f / x.l[0];
+        const float inv = kv_inverse(x.l[0], t.nb);
         uint16_t* op = a.out + (t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + g * 4;
 #pragma unroll
         for (int y = 0; y < NO; ++y) {
@@ -1127,7 +1133,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
             }
           } else {
             const int q = t.r0 + r;
-            const float v = l0 == 0.f ? 0.f : o0 * (1.0f / l0);
+            const float v = o0 * kv_inverse(l0, t.nb);
             a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
           }
         }
@@ -1218,7 +1224,7 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
     const int e = threadIdx.x + x * 256;
     if (e >= t.rows * HD) break;
     const int r = e / HD, d = e % HD, q = t.r0 + r;
-    const float v = segs == 0 || sum[r] == 0.f ? 0.f : o[x] * (1.0f / sum[r]);
+    const float v = segs == 0 ? 0.f : o[x] * kv_inverse(sum[r], t.nb);
     a.out[(t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + d] = f2act(v, a.out_act);
   }
 }
@@ -1535,7 +1541,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_kv_attend_rows(KvAtte
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int r = w * 32 + x * 16 + c16;
-      const float lw = swap_add(l[x]), inv = lw == 0.f ? 0.f : 1.0f / lw;
+      const float lw = swap_add(l[x]), inv = kv_inverse(lw, t.nb);
       if (r < t.rows) {
         const int q = t.r0 + r;
         uint16_t* op = a.out + (t.s.row0 + q / rep) * a.out_ld + (h * rep + q % rep) * HD + g * 4;

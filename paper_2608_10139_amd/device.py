@@ -397,9 +397,9 @@ class DeviceKvCache:
         self.n_kv_heads, self.head_dim, self.dtype = int(n_kv_heads), int(head_dim), dtype
         nb, nt = int(n_blocks), int(n_tails)
         size = (nb, self.n_kv_heads, B.AIQ_KV_BLOCK * self.head_dim)
-        # zeros, so that blocks that were never written read back as zeros
-        self.k = torch.zeros(size, dtype=torch.uint8, device=self.device)
-        self.v = torch.zeros(size, dtype=torch.uint8, device=self.device)
+        # whole numbers of 0 (stored with 128 added), so that blocks that were never written hold zeros
+        self.k = torch.full(size, 128, dtype=torch.uint8, device=self.device)
+        self.v = torch.full(size, 128, dtype=torch.uint8, device=self.device)
         self.k_scale = torch.zeros(size[:2], dtype=torch.float32, device=self.device)
         self.v_scale = torch.zeros(size[:2], dtype=torch.float32, device=self.device)
         self.tail = torch.zeros((nt, 2, self.n_kv_heads, B.AIQ_KV_BLOCK, self.head_dim), dtype=dtype, device=self.device)

@@ -570,3 +570,46 @@ def test_single_rows_complete_blocks_in_any_group(n, hd):
     for p, q in zip(c.cache.read(c.batch(lens + 6, lens + 6)), d.cache.read(d.batch(lens + 6, lens + 6))):
         assert torch.equal(p, q)
     c.ok()
+
+
+# (sequences, new rows of each or None for one by `cu` NULL, heads, K/V heads, head_dim): a workgroup per item, segments in
+# workgroups of their own, waves alone, tiles of 16 rows, tiles of 128
+FORMS = [([40, 100, 96], None, 6, 2, 64), ([3000], None, 8, 2, 128), ([50] * 1100, None, 4, 2, 64),
+         ([40, 100, 96], 9, 6, 2, 64), ([90] * 60, 33, 8, 2, 128)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("lens,new,heads,kv,hd", FORMS, ids=lambda x: str(x)[:12])
+def test_a_query_whose_scores_are_all_minus_infinity(lens, new, heads, kv, hd, dtype):
+    """Its softmax is not a number, as by the formula; the other queries are as without it."""
+    say("case: infinite query", len(lens), new, heads, kv, hd, dtype)
+    c = Case(lens, heads, kv, hd, dtype, 71)
+    for k in c.k:
+        k[:, :, 0] = -1.0
+    lens, ones = np.array(lens), np.full(len(lens), new or 1)
+    c.write(lens, lens)
+    b, q = c.batch(lens, ones, single=new is None), c.rows("q", lens, ones)
+    want = c.cache.attend(b, q)
+    poisoned = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+    poisoned[::2, 1] = True
+    poisoned[-1, -1] = True
+    q = q.clone()
+    q[..., 0] = torch.where(poisoned, torch.inf, q[..., 0])
+    out = c.cache.attend(b, q)
+    assert torch.isnan(out[poisoned]).all()
+    top = max(float(v.abs().max()) for v in c.v)   # (a tile's rows share when their references move: two results within their bounds)
+    tol = 2 * ((U[dtype] + 2.0 ** -14) * top + U[dtype] * want.double().abs() + 1e-7)
+    assert bool(((out.double() - want.double()).abs() <= tol)[~poisoned].all())
+    c.ok()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("lens,new,heads,kv,hd", FORMS, ids=lambda x: str(x)[:12])
+def test_blocks_that_were_never_written_hold_zeros(lens, new, heads, kv, hd, dtype):
+    say("case: nothing written", len(lens), new, heads, kv, hd, dtype)
+    c = Case(lens, heads, kv, hd, dtype, 75)
+    ones = np.full(len(lens), new or 1)
+    for x in c.cache.read(c.batch(lens, lens)):
+        assert bool((x == 0).all())
+    assert bool((c.cache.attend(c.batch(lens, ones, single=new is None), c.rows("q", lens, ones)) == 0).all())
+    c.ok()
