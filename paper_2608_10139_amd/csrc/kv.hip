@@ -962,7 +962,8 @@ struct KvWave {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       pf.u[e] = BF ? f2bf(p[0][0][e]) : f2h(p[0][0][e]);
-      if (several && p[0][0][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[0] = __uint_as_float(0x7FC00000u);
+      const int at = (e / 4) * 16 + g * 4 + e % 4;
+      if (several && tok0 + at <= pos && bad[at]) l[0] = __uint_as_float(0x7FC00000u);   // (whatever it weighs: 0 times it is NaN)
     }
     // lane 4 a + b of a 16-lane group receives element b of the pieces that lanes a, a + 4, .. address
     lds_u16* const vl = (lds_u16*)(vt);
@@ -1525,7 +1526,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void k_kv_attend_rows(KvAtte
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             pf.u[e] = BF ? f2bf(p[0][x][e]) : f2h(p[0][x][e]);
-            if (p[0][x][e] > 0.f && bad[(e / 4) * 16 + g * 4 + e % 4]) l[x] = __uint_as_float(0x7FC00000u);
+            const int at = (e / 4) * 16 + g * 4 + e % 4;
+            if (tok0 + at <= pos[x] && bad[at]) l[x] = __uint_as_float(0x7FC00000u);   // (whatever it weighs: 0 times it is NaN)
           }
 #pragma unroll
           for (int f = 0; f < FR; ++f)

@@ -613,3 +613,21 @@ def test_blocks_that_were_never_written_hold_zeros(lens, new, heads, kv, hd, dty
         assert bool((x == 0).all())
     assert bool((c.cache.attend(c.batch(lens, ones, single=new is None), c.rows("q", lens, ones)) == 0).all())
     c.ok()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,new", [(3, None), (3, 5), (60, 40)])
+def test_an_infinite_value_of_a_seen_token_without_weight(n, new, dtype):
+    """A token of the tail whose weight is 0 in 32 bits: 0 times its infinite value is not a number, in every form."""
+    say("case: infinite value without weight", n, new, dtype)
+    lens, ones, at = np.full(n, 90), np.full(n, new or 1), 86
+    c = Case(lens, 8, 2, 64, dtype, 74)
+    for q, k, v in zip(c.q, c.k, c.v):
+        q[:], k[:] = 20.0, 0.0
+        k[at] = -20.0        # a score of -3,200
+        v[at, 1, 7] = float("inf")
+    c.write(lens, lens)
+    out = c.cache.attend(c.batch(lens, ones, single=new is None), c.rows("q", lens, ones)).view(n, -1, 8, 64)
+    seen = 90 - at if new else 1
+    assert torch.isnan(out[:, -seen:, 4:, 7]).all()
+    assert torch.isfinite(out[:, -seen:, :4]).all() and torch.isfinite(out[:, :-seen]).all()
