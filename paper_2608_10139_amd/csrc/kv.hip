@@ -983,6 +983,9 @@ struct KvWave {
   }
 };
 
+// floats of a state of `rows` rows in the waves alone: [rows][hd], [2][rows], a multiple of 4
+static __host__ __device__ int alone_state(int rows, int hd) { return (rows * (hd + 2) + 3) / 4 * 4; }
+
 // NW = 4: a workgroup per (tile, K/V head), or with SPLIT per segment of one.
 // NW = 1: a wave per (tile, K/V head) takes the four shares of each segment one after another:
 // the same sums, without the exchange.
@@ -998,7 +1001,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
   float* sm = so + (NW == 4 ? 4 * slot_rows * HD : 0);   // [4][rows]
   float* sl = sm + (NW == 4 ? 4 * slot_rows : 0);
   // of the earlier segments, where there are several: [rows][HD], [2][2][rows]; NW = 1: of the earlier shares
-  // [rows][HD], [2][rows], then of the earlier segments the same
+  // [rows][HD], [2][rows], then of the earlier segments the same (alone_state floats each, so that 16-byte accesses are aligned)
   float* state = sl + (NW == 4 ? 4 * slot_rows : 0);
   const KvCache& c = a.c;
   const int n = kv_count(a.b);
@@ -1021,16 +1024,17 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 3 : 2) void k_kv_attend(KvAttend
     Wave x(a, t, h, rep, vt, bad);
     if (NW == 1) {
       // states between shares and between segments: LDS (few rows; registers for them would cost a wave per SIMD)
-      const int stride = slot_rows * (HD + 2);
+      const int stride = alone_state(slot_rows, HD);
       auto fold = [&](bool any, const float* st) {   // the state st (none: !any), then this one, into (x.m, x.l, x.o)
-        const float m0 = any ? st[slot_rows * HD + c16] : -INFINITY, l0 = any ? st[slot_rows * HD + slot_rows + c16] : 0.f;
+        const bool is = any && c16 < t.rows;   // (a tile has slot_rows rows at most: a state holds no more)
+        const float m0 = is ? st[slot_rows * HD + c16] : -INFINITY, l0 = is ? st[slot_rows * HD + slot_rows + c16] : 0.f;
         const float mn = fmaxf(m0, x.m[0]), ref = mn == -INFINITY ? 0.f : mn;
         const float e0 = __builtin_amdgcn_exp2f(m0 - ref), e1 = __builtin_amdgcn_exp2f(x.m[0] - ref);
         x.l[0] = fmaf(x.l[0], e1, l0 * e0);
 #pragma unroll
         for (int y = 0; y < NO; ++y) {
           f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
-          if (any && c16 < t.rows) z = *reinterpret_cast<const f32x4*>(st + c16 * HD + y * 16 + g * 4);
+          if (is) z = *reinterpret_cast<const f32x4*>(st + c16 * HD + y * 16 + g * 4);
 #pragma unroll
           for (int e = 0; e < 4; ++e) x.o[0][y][e] = fmaf(x.o[0][y][e], e1, z[e] * e0);
         }
@@ -1639,8 +1643,8 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t s) {
   }
   const int64_t cap = !a.b.n_ptr ? 1 << 20 : k.alone ? 1 << 16 : 1 << 14;   // (a bound from the host only: the sequences may be few)
   const dim3 grid(static_cast<unsigned>(items < cap ? items : cap));
-  const int state = k.alone ? 2 * (a.c.hd + 2) : 4 * (a.c.hd + 2) + (!k.split && k.n_seg > 1 ? a.c.hd + 4 : 0);   // per row
-  const size_t lds = static_cast<size_t>(k.rows) * state * 4;
+  const int state = 4 * (a.c.hd + 2) + (!k.split && k.n_seg > 1 ? a.c.hd + 4 : 0);   // per row, of four waves
+  const size_t lds = static_cast<size_t>(k.alone ? 2 * alone_state(k.rows, a.c.hd) : k.rows * state) * 4;
 #define AIQ_KV_ATTEND(HD_, BF_, SP_, NW_) \
   hipLaunchKernelGGL((k_kv_attend<HD_, BF_, SP_, NW_>), grid, dim3(64 * NW_), lds, s, a, k.tiles, k.n_seg, k.rows)
 #define AIQ_KV_ATTEND_BF(HD_, BF_)                       \

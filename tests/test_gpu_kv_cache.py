@@ -631,3 +631,25 @@ def test_an_infinite_value_of_a_seen_token_without_weight(n, new, dtype):
     seen = 90 - at if new else 1
     assert torch.isnan(out[:, -seen:, 4:, 7]).all()
     assert torch.isfinite(out[:, -seen:, :4]).all() and torch.isfinite(out[:, :-seen]).all()
+
+
+@pytest.mark.parametrize("heads,kv,hd", [(4, 4, 64), (12, 4, 64), (12, 4, 128), (20, 4, 64), (72, 4, 64)])
+def test_waves_alone_over_several_segments(heads, kv, hd):
+    """Groups of 1, 3, 5 and 18 (two tiles) heads, sequences of up to three segments of 512 tokens: within the bound, and the bits of the
+    sequence by itself (a workgroup's four waves)."""
+    say("case: waves alone, several segments", heads, kv, hd)
+    n = 2400
+    lens = np.full(n, 2)
+    lens[[3, 700, 2399]] = 1400, 513, 1030
+    c = Case(lens, heads, kv, hd, torch.float16, 76, paged=False)
+    c.write(lens, lens)
+    ones = np.ones(n, np.int64)
+    q = c.rows("q", lens, ones)
+    out = c.cache.attend(c.batch(lens, ones, single=True), q)
+    for i in (3, 700, 2399):
+        alone = c.cache.batch(i32(lens[i:i + 1]), i32(c.start[i:i + 2]), 1024 if lens[i] < 1024 else 1400, tail_ids=i32([i]))
+        assert torch.equal(c.cache.attend(alone, q[i:i + 1])[0], out[i])
+        want, top = R.attend(c.q[i][-1:].float().numpy(), *c.held(i), [lens[i] - 1])
+        tol = (2.0 ** -11 + 2.0 ** -14) * top[:, :, None] + 2.0 ** -11 * np.abs(want) + 1e-7
+        assert np.all(np.abs(out[i:i + 1].double().cpu().numpy() - want) <= tol)
+    c.ok()
