@@ -641,7 +641,8 @@ aiq_status aiq_kv_attend_workspace_size(const aiq_kv_cache* cache, const aiq_kv_
  * rows.  The row of an empty slot (len[i] = 0) becomes zero.  A query sees a
  * token only through the scale of its block: an infinity or NaN in the block
  * of a visible token reaches the output, one in later blocks does not.  With
- * one row per sequence the result does not depend on the other sequences.
+ * one row per sequence at most (cu NULL, or n_rows no more than n_seq) the
+ * result does not depend on the other sequences.
  * workspace: 256-byte aligned, aiq_kv_attend_workspace_size bytes (NULL where
  * that is 0); calls that may overlap need one each.  Errors: AIQ_EINVAL (as
  * aiq_kv_write; n_heads not a multiple of n_kv_heads), AIQ_EUNSUPPORTED (as

@@ -1585,7 +1585,9 @@ static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
   // against 56.  Where the tiles of 16 are few they run at once, four waves to a tile's keys: 16 sequences of 2,000 with
   // 16 (512 and 640 of them) 65 against 47 and 48 against 37, with 32 (896, 1,152) 67 against 81 and 52 against 57; 4 of
   // 4,000 with 64 (416, 544) 116 against 83 and 84 against 64, with 128 (800, 1,056) 121 against 137 and 87 against 93.
-  s.many = b.cu && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY && s.tiles * c.n_kv >= 768;
+  // (One row per sequence stays with the tiles of 16 whatever its heads: their order of sums is the keys' alone.)
+  s.many = b.cu && b.n_rows > b.n_seq && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY &&
+           s.tiles * c.n_kv >= 768;
   if (s.many) {
     s.tiles = big;
     return s;

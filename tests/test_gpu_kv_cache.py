@@ -653,3 +653,23 @@ def test_waves_alone_over_several_segments(heads, kv, hd):
         tol = (2.0 ** -11 + 2.0 ** -14) * top[:, :, None] + 2.0 ** -11 * np.abs(want) + 1e-7
         assert np.all(np.abs(out[i:i + 1].double().cpu().numpy() - want) <= tol)
     c.ok()
+
+
+@pytest.mark.parametrize("n", [150, 400])
+def test_one_row_per_sequence_and_many_heads_does_not_depend_on_the_others(n):
+    """64 query heads on one K/V head, the rows given by cu: the bits of a sequence by itself."""
+    say("case: 64 heads on one", n)
+    lens = np.random.default_rng(72).integers(1, 500, n)
+    lens[5] = 480
+    c = Case(lens, 64, 1, 64, torch.float16, 73)
+    c.write(lens, lens)
+    ones = np.ones(n, np.int64)
+    q = c.rows("q", lens, ones)
+    many = c.cache.attend(c.batch(lens, ones), q)
+    assert torch.equal(many, c.cache.attend(c.batch(lens, ones, single=True), q))
+    for i in (0, 5, n - 1):
+        s, e = c.start[i], c.start[i + 1]
+        alone = c.cache.batch(i32([lens[i]]), i32([0, e - s]), 500, cu=i32([0, 1]), blk_ids=c.blk_ids[s:e].contiguous(),
+                              tail_ids=c.tail_ids[i:i + 1].contiguous())
+        assert torch.equal(c.cache.attend(alone, q[i:i + 1])[0], many[i])
+    c.ok()
