@@ -51,7 +51,7 @@
 extern "C" {
 #endif
 
-#define AIQ_ABI_VERSION 7
+#define AIQ_ABI_VERSION 8
 
 typedef enum aiq_status {
   AIQ_OK = 0,
@@ -583,7 +583,8 @@ typedef struct aiq_kv_cache {
  * that a call writes belongs to one sequence alone.  Rows before the first and
  * past the last sequence's are not touched.
  * A sequence whose numbers do not fit (len[i] above max_len or its blocks, more
- * rows than tokens, a tail or block number out of range) sets
+ * rows than tokens, a tail or block number out of range, full blocks whose
+ * entries lie past n_blk_ids) sets
  * AIQ_DEV_KV_RANGE in *status, and nothing of it is read or written out of
  * bounds; its outputs are unspecified.
  */
@@ -597,6 +598,7 @@ typedef struct aiq_kv_batch {
   const int32_t* blk_ids;    /* device, or NULL */
   const int32_t* tail_ids;   /* device [n_seq], or NULL */
   int64_t* status;           /* device word that AIQ_DEV_KV_RANGE is set in, or NULL */
+  int64_t n_blk_ids;         /* entries of blk_ids; 0: as many as blk_start needs, unchecked */
 } aiq_kv_batch;
 
 /*

@@ -13,7 +13,7 @@ import os
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libaiq.so")
 
-AIQ_ABI_VERSION = 7   # the struct layouts below
+AIQ_ABI_VERSION = 8   # the struct layouts below
 AIQ_OK, AIQ_EINVAL, AIQ_EUNSUPPORTED, AIQ_ENOSPC, AIQ_EHIP, AIQ_ENOMEM = 0, -1, -2, -3, -4, -5
 AIQ_I8, AIQ_I16, AIQ_I32, AIQ_F32, AIQ_BF16, AIQ_F16 = 1, 2, 3, 4, 5, 6
 AIQ_LT, AIQ_LE, AIQ_GT, AIQ_GE, AIQ_EQ, AIQ_NE, AIQ_IN = range(7)
@@ -117,7 +117,7 @@ class aiq_kv_cache(C.Structure):
 class aiq_kv_batch(C.Structure):
     _fields_ = [("n_seq", C.c_int32), ("max_len", C.c_int32), ("n_rows", C.c_int64), ("len", C.c_void_p),
                 ("cu", C.c_void_p), ("blk_start", C.c_void_p), ("blk_ids", C.c_void_p), ("tail_ids", C.c_void_p),
-                ("status", C.c_void_p)]
+                ("status", C.c_void_p), ("n_blk_ids", C.c_int64)]
 
 
 EXPORTS = ("aiq_plan_create", "aiq_workspace_size", "aiq_plan_passes", "aiq_plan_chunk_tokens",

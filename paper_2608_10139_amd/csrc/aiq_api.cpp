@@ -415,6 +415,7 @@ KvBatch kv8_batch(const aiq_plan* p, void* ws, const Layout& L, const int64_t* n
   b.n_ptr = n_seq;
   b.len = at<int32_t>(ws, L.plen);
   b.blk_start = at<int32_t>(ws, L.pblk);
+  b.n_ids = INT32_MAX;
   b.status = ctr + C_STATUS;
   return b;
 }
@@ -1514,7 +1515,7 @@ aiq_status kv_args(const aiq_kv_cache* c, const aiq_kv_batch* b, KvCache* kc, Kv
   for (const void* p : {c->k, c->v, c->tail})
     if (reinterpret_cast<uintptr_t>(p) % 16) return AIQ_EINVAL;
   if (reinterpret_cast<uintptr_t>(c->k_scale) % 4 || reinterpret_cast<uintptr_t>(c->v_scale) % 4) return AIQ_EINVAL;
-  if (b->n_seq < 0 || b->n_rows < 0 || b->n_rows > INT32_MAX || b->max_len < 0) return AIQ_EINVAL;
+  if (b->n_seq < 0 || b->n_rows < 0 || b->n_rows > INT32_MAX || b->max_len < 0 || b->n_blk_ids < 0) return AIQ_EINVAL;
   if (b->n_seq > 0 && (!b->len || !b->blk_start)) return AIQ_EINVAL;
   if (!b->cu && b->n_rows != b->n_seq) return AIQ_EINVAL;
   if (reinterpret_cast<uintptr_t>(b->status) % 8) return AIQ_EINVAL;
@@ -1538,6 +1539,7 @@ aiq_status kv_args(const aiq_kv_cache* c, const aiq_kv_batch* b, KvCache* kc, Kv
   kb->cu = b->cu;
   kb->blk_start = b->blk_start;
   kb->blk_ids = b->blk_ids;
+  kb->n_ids = b->blk_ids && b->n_blk_ids ? static_cast<int32_t>(std::min<int64_t>(b->n_blk_ids, INT32_MAX)) : INT32_MAX;
   kb->tail_ids = b->tail_ids;
   kb->status = b->status;
   return AIQ_OK;

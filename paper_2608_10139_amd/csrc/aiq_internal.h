@@ -512,6 +512,7 @@ struct KvBatch {
   int32_t n_pre;
   const int32_t* blk_start;
   const int32_t* blk_ids;
+  int32_t n_ids;             // its entries; INT32_MAX where blk_ids is null or the caller did not say
   const int32_t* tail_ids;
   int64_t* status;
 };

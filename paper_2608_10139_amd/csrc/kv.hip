@@ -87,14 +87,14 @@ __device__ __forceinline__ bool kv_seq(const KvCache& c, const KvBatch& b, const
   s.tail = uniform(r.tail());
   const bool uses_tail = s.len % KVB != 0 || (s.len - s.n) % KVB != 0;
   if (s.len < s.n || s.len > b.max_len || e0 < 0 || (c.n_blocks == 0 && s.len >= KVB) || (e1 - e0) * KVB < s.len ||
-      (uses_tail && (s.tail < 0 || s.tail >= c.n_tails))) {
+      e0 + s.len / KVB > b.n_ids || (uses_tail && (s.tail < 0 || s.tail >= c.n_tails))) {
     kv_flag(b);
     return false;
   }
   return true;
 }
 
-// Block number of entry e, or -1 (flagged) where it is outside the cache.
+// Block number of entry e (of a full block of a sequence that kv_seq has let through), or -1 (flagged) where it is outside the cache.
 __device__ __forceinline__ int kv_block(const KvCache& c, const KvBatch& b, int e) {
   const int id = b.blk_ids ? b.blk_ids[e] : e;
   if (id >= 0 && id < c.n_blocks) return id;

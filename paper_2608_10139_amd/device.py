@@ -427,10 +427,13 @@ class DeviceKvCache:
             _need(t, self.device, torch.int32, what)
             if not t.is_contiguous() or (want is not None and t.numel() != want):
                 raise ValueError(f"{what}: {want} contiguous values wanted, got {tuple(t.shape)}")
+        if blk_ids is not None and not blk_ids.numel():   # (no address to tell it from None: one entry that is no block)
+            blk_ids = torch.full((1,), -1, dtype=torch.int32, device=self.device)
         b = B.aiq_kv_batch()
         b.n_seq, b.max_len = n, int(max_len)
         b.n_rows = n if cu is None else int(cu[-1].item()) if n_rows is None else int(n_rows)
         b.len, b.cu, b.blk_start, b.blk_ids, b.tail_ids = (_ptr(t) for t in (length, cu, blk_start, blk_ids, tail_ids))
+        b.n_blk_ids = 0 if blk_ids is None else blk_ids.numel()
         b.status = _ptr(self.status)
         return KvBatch(b, (length, blk_start, cu, blk_ids, tail_ids))
 

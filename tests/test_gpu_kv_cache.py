@@ -673,3 +673,28 @@ def test_one_row_per_sequence_and_many_heads_does_not_depend_on_the_others(n):
                               tail_ids=c.tail_ids[i:i + 1].contiguous())
         assert torch.equal(c.cache.attend(alone, q[i:i + 1])[0], many[i])
     c.ok()
+
+
+def test_blocks_past_the_end_of_the_list_are_flagged_and_left_out():
+    say("case: short lists of blocks")
+    lens, ones = np.array([70, 40]), np.ones(2, np.int64)
+    c = Case(lens, 2, 2, 64, torch.float16, 77, paged=False)
+    c.write(lens, lens)
+    q = c.rows("q", lens, ones)
+    want = c.cache.attend(c.batch(lens, ones), q)
+    # sequence 1's full block is entry 3, sequence 0's are entries 0 and 1; the tails' entries are not read
+    for ids, good in (([0, 1, 2, 3], [0, 1]), ([0, 1, 2], [0]), ([0, 1], [0]), ([0], []), ([], [])):
+        for cu in (None, i32([0, 1, 2])):
+            say("  ", ids, cu is None)
+            kv = [t.clone() for t in (c.cache.k, c.cache.v, c.cache.k_scale, c.cache.v_scale, c.cache.tail)]
+            b = c.cache.batch(i32(lens), i32([0, 3, 5]), 70, cu=cu, blk_ids=i32(ids))
+            out = c.cache.attend(b, q)
+            for i in good:
+                assert torch.equal(out[i], want[i])
+            assert int(c.cache.status.item()) == (0 if len(good) == 2 else B.AIQ_DEV_KV_RANGE)
+            c.cache.read(b)
+            c.cache.write(b, c.rows("k", lens, ones), c.rows("v", lens, ones))   # (its last row again)
+            for x, y in zip(kv, (c.cache.k, c.cache.v, c.cache.k_scale, c.cache.v_scale, c.cache.tail)):
+                assert torch.equal(x, y)
+            assert int(c.cache.status.item()) == (0 if len(good) == 2 else B.AIQ_DEV_KV_RANGE)
+            c.cache.status.zero_()

@@ -226,3 +226,17 @@ def test_8_bit_plans_out_of_range():
     t = table()
     t.max_list_len = (1 << 31) - 2           # lengths and generated tokens pass 32 bits
     assert status(t=t) == B.AIQ_EUNSUPPORTED
+
+
+def test_entries_of_the_block_list():
+    n = C.c_size_t()
+    for bad in (-1, -(1 << 40)):
+        b = batch(blk_ids=FAKE, n_blk_ids=bad)
+        assert write(cache(), b) == write(cache(), b, read=True) == attend(cache(), b) == B.AIQ_EINVAL
+        assert B.load().aiq_kv_attend_workspace_size(C.byref(cache()), C.byref(b), 8, C.byref(n)) == B.AIQ_EINVAL
+    c = DeviceKvCache(4, 2, 2, 64, device="cpu")
+    i = lambda *x: torch.tensor(x, dtype=torch.int32)   # noqa: E731
+    assert c.batch(i(5, 6), i(0, 2, 4), 64).struct.n_blk_ids == 0
+    assert c.batch(i(5, 6), i(0, 2, 4), 64, blk_ids=i(3, 2, 1)).struct.n_blk_ids == 3
+    b = c.batch(i(5, 6), i(0, 2, 4), 64, blk_ids=i())   # a list without entries is not the numbers themselves
+    assert b.struct.blk_ids and b.struct.n_blk_ids == 1
