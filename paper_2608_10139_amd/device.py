@@ -372,14 +372,24 @@ def _need(t: torch.Tensor, device, dtype, what: str) -> torch.Tensor:
 
 
 class KvBatch:
-    """The sequences of a call on a DeviceKvCache (see DeviceKvCache.batch)."""
+    """The sequences of a call on a DeviceKvCache (see DeviceKvCache.batch), or on several: the caches of a model's layers, say."""
 
-    def __init__(self, struct: B.aiq_kv_batch, keep: tuple):
+    def __init__(self, struct: B.aiq_kv_batch, keep: tuple, shape: tuple):
         self.struct = struct
+        self.shape = shape    # K/V heads and head size of the cache that made it
         self.keep = keep      # the tensors that the struct points into
         self.device = keep[0].device
         self.n_rows = int(struct.n_rows)
-        self.ws_bytes = {}    # attention workspace by query heads
+        self.ws_bytes = {}    # attention workspace by query heads, for caches of the first one's shape; for others:
+        self.ws_other = {}    # by (query heads, K/V heads, head size)
+
+    def of(self, cache: "DeviceKvCache") -> B.aiq_kv_batch:
+        """The struct, with the status word of the cache that a call is on."""
+        if self.struct.status == cache.status.data_ptr():
+            return self.struct
+        b = B.aiq_kv_batch.from_buffer_copy(self.struct)
+        b.status = _ptr(cache.status)
+        return b
 
 
 class DeviceKvCache:
@@ -418,7 +428,9 @@ class DeviceKvCache:
         numbers themselves), with tail tail_ids[i] (None: i).  All int32
         tensors on the cache's device; they may change between calls, within
         max_len tokens and n_rows rows (None with cu: cu's last value is read
-        back once, here).  The tensors are kept, not copied."""
+        back once, here).  The tensors are kept, not copied.  A batch may be used
+        with other caches that have these blocks and tails, of any shape; each
+        call sets the status of the cache that it is made on."""
         n = int(length.numel())
         for t, want, what in ((length, n, "length"), (blk_start, n + 1, "blk_start"), (cu, n + 1, "cu"),
                               (blk_ids, None, "blk_ids"), (tail_ids, n, "tail_ids")):
@@ -435,7 +447,8 @@ class DeviceKvCache:
         b.len, b.cu, b.blk_start, b.blk_ids, b.tail_ids = (_ptr(t) for t in (length, cu, blk_start, blk_ids, tail_ids))
         b.n_blk_ids = 0 if blk_ids is None else blk_ids.numel()
         b.status = _ptr(self.status)
-        return KvBatch(b, (length, blk_start, cu, blk_ids, tail_ids))
+        return KvBatch(b, (length, blk_start, cu, blk_ids, tail_ids, self.status),
+                       (self.n_kv_heads, self.head_dim))
 
     def _mine(self, batch: KvBatch) -> int:
         """The batch's rows; its tensors must be on the cache's device."""
@@ -460,7 +473,7 @@ class DeviceKvCache:
         n = self._mine(batch)
         ks, vs = (self._rows(t, n, self.n_kv_heads, w) for t, w in ((k, "k"), (v, "v")))
         with _on(self.device, stream) as s:
-            B.aiq_kv_write(self.struct, batch.struct, _ptr(k), ks, _ptr(v), vs, s)
+            B.aiq_kv_write(self.struct, batch.of(self), _ptr(k), ks, _ptr(v), vs, s)
 
     def read(self, batch: KvBatch, stream=None) -> tuple:
         """The batch's rows as the cache holds them: (k, v)."""
@@ -468,7 +481,7 @@ class DeviceKvCache:
         with _on(self.device, stream) as s:
             k, v = (torch.empty((n, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device)
                     for _ in range(2))
-            B.aiq_kv_read(self.struct, batch.struct, _ptr(k), w, _ptr(v), w, s)
+            B.aiq_kv_read(self.struct, batch.of(self), _ptr(k), w, _ptr(v), w, s)
         return k, v
 
     def attend(self, batch: KvBatch, q: torch.Tensor, out: torch.Tensor | None = None,
@@ -482,14 +495,16 @@ class DeviceKvCache:
         dtype = out.dtype if out is not None else out_dtype or self.dtype
         if dtype not in (torch.float16, torch.bfloat16):
             raise ValueError(f"out is float16 or bfloat16, not {dtype}")
-        need = batch.ws_bytes.get(heads)
+        shape = (self.n_kv_heads, self.head_dim)
+        sizes, key = (batch.ws_bytes, heads) if shape == batch.shape else (batch.ws_other, (heads, *shape))
+        need = sizes.get(key)
         if need is None:
-            need = batch.ws_bytes[heads] = B.aiq_kv_attend_workspace_size(self.struct, batch.struct, heads)
+            need = sizes[key] = B.aiq_kv_attend_workspace_size(self.struct, batch.struct, heads)
         with _on(self.device, stream) as s:   # the workspace belongs to the stream that uses it
             if out is None:
                 out = torch.empty(q.shape, dtype=dtype, device=self.device)
             ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-            B.aiq_kv_attend(self.struct, batch.struct, _ptr(q), qs, heads, _ptr(out), heads * self.head_dim,
+            B.aiq_kv_attend(self.struct, batch.of(self), _ptr(q), qs, heads, _ptr(out), heads * self.head_dim,
                             _TORCH_DTYPE[dtype], _ptr(ws), need, s)
         return out
 

@@ -698,3 +698,17 @@ def test_blocks_past_the_end_of_the_list_are_flagged_and_left_out():
                 assert torch.equal(x, y)
             assert int(c.cache.status.item()) == (0 if len(good) == 2 else B.AIQ_DEV_KV_RANGE)
             c.cache.status.zero_()
+
+
+def test_a_batch_on_two_caches():
+    """Caches of other heads and head sizes behind one batch: each call's workspace, and flags in the status of its cache."""
+    say("case: a batch on two caches")
+    lens = [6000, 37]
+    c, d = Case(lens, 8, 1, 64, torch.float16, 78, paged=False), Case(lens, 8, 8, 128, torch.float16, 79, paged=False)
+    b, one = c.batch(lens, lens), c.batch(lens, [1, 1], single=True)
+    for x in (c, d, c):
+        x.cache.write(b, x.rows("k", lens, lens), x.rows("v", lens, lens))
+        x.check_attend(lens, [1, 1], x.cache.attend(one, x.rows("q", lens, [1, 1])))
+    bad = c.cache.batch(i32([7000, 37]), c.blk_start, 7000)
+    d.cache.attend(bad, d.rows("q", lens, [1, 1]))
+    assert int(c.cache.status.item()) == 0 and int(d.cache.status.item()) == B.AIQ_DEV_KV_RANGE

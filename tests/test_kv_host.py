@@ -240,3 +240,39 @@ def test_entries_of_the_block_list():
     assert c.batch(i(5, 6), i(0, 2, 4), 64, blk_ids=i(3, 2, 1)).struct.n_blk_ids == 3
     b = c.batch(i(5, 6), i(0, 2, 4), 64, blk_ids=i())   # a list without entries is not the numbers themselves
     assert b.struct.blk_ids and b.struct.n_blk_ids == 1
+
+
+def test_a_batch_on_caches_of_other_shapes(monkeypatch):
+    """Workspace by the cache's shape, flags in its own status word, which the batch keeps."""
+    from paper_2608_10139_amd import device as D
+
+    class On:
+        def __init__(self, device, stream):
+            pass
+
+        def __enter__(self):
+            return 0
+
+        def __exit__(self, *e):
+            pass
+
+    calls = []
+    monkeypatch.setattr(D, "_on", On)
+    for f in ("aiq_kv_write", "aiq_kv_read"):
+        monkeypatch.setattr(B, f, lambda c, b, *a: calls.append((c, b.status, 0, 0)))
+    monkeypatch.setattr(B, "aiq_kv_attend", lambda c, b, q, qs, heads, o, os, dt, ws, n, s: calls.append((c, b.status, n, heads)))
+    i = lambda *x: torch.tensor(x, dtype=torch.int32)   # noqa: E731
+    one, two, three = (DeviceKvCache(256, 1, kv, hd, device="cpu") for kv, hd in ((2, 64), (8, 128), (2, 64)))
+    b = one.batch(i(8000), i(0, 256), 8192)
+    needs = []
+    for c in (one, two, three, one):
+        kv = torch.zeros(1, c.n_kv_heads, c.head_dim, dtype=torch.float16)
+        c.write(b, kv, kv)
+        c.read(b)
+        c.attend(b, torch.zeros(1, 8, c.head_dim, dtype=torch.float16))
+        want = B.aiq_kv_attend_workspace_size(c.struct, b.struct, 8)
+        assert calls[-1][2:] == (want, 8)
+        assert [x[1] for x in calls[-3:]] == [c.status.data_ptr()] * 3
+        needs.append(want)
+    assert needs[0] == needs[2] == needs[3] < needs[1]
+    assert any(t is one.status for t in b.keep)
