@@ -607,8 +607,10 @@ typedef struct aiq_kv_batch {
  * head_dim elements of the cache's dtype, k_ld and v_ld elements apart (so
  * they may be columns of q|k|v rows); 16-byte aligned, the strides multiples
  * of 8.  Appending must be in order: the earlier len[i] - n tokens of
- * a sequence are in the cache.  Writing a row again has the same result as
- * long as no later block has been begun.
+ * a sequence are in the cache.  Writing rows again has the same result where
+ * the first of them begins a block or lies in one that is not full, or where
+ * the call that filled the block is repeated before the next one is begun (a
+ * full block's earlier tokens may never have been in the tail, or no longer be).
  * Errors: AIQ_EINVAL (NULL pointer, negative count, head_dim, stride or
  * alignment, cu NULL with n_rows != n_seq), AIQ_EUNSUPPORTED (dtype; more
  * than 2^16 heads, 2^26 sequences or 2^30 tokens in one), AIQ_EHIP.  Nothing

@@ -712,3 +712,30 @@ def test_a_batch_on_two_caches():
     bad = c.cache.batch(i32([7000, 37]), c.blk_start, 7000)
     d.cache.attend(bad, d.rows("q", lens, [1, 1]))
     assert int(c.cache.status.item()) == 0 and int(d.cache.status.item()) == B.AIQ_DEV_KV_RANGE
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_rows_written_again(hd):
+    """From a block's first token on, inside a block that is not full, or by the call that filled one: the same bytes and tails."""
+    say("case: rows written again", hd)
+    #  sequence:        0   1   2   3   4   5   6
+    lens = np.array([  50, 50, 64, 32, 40, 33, 20])
+    c = Case(lens, 2, 2, hd, torch.bfloat16, 80)
+    first = np.array([ 10, 50, 45, 10,  0, 32,  5])   # tokens of a first call, the others come in a second
+    c.write(first, first)
+    c.write(lens, lens - first)
+    names = ("k", "v", "k_scale", "v_scale", "tail")
+    before = [getattr(c.cache, x).clone() for x in names]
+    # the end of a tail; from a block's start over its end; the filling call; the filling call; a tail's one row; the same; all
+    again = np.array([ 3, 50, 19, 22,  1,  1, 20])
+    c.write(lens, again)
+    # whole blocks in the middle, the later tokens left as they are
+    c.write(np.array([32, 32, 32, 32, 32, 32, 0]), np.array([32, 32, 32, 32, 32, 32, 0]))
+    for x, y in zip(names, before):
+        assert torch.equal(getattr(c.cache, x), y), x
+    c.write(lens, np.array([1, 1, 0, 0, 1, 1, 1]))
+    one = lens % BLOCK != 0
+    c.write(np.where(one, lens, 0), np.ones(7, np.int64) * one, single=False)
+    for x, y in zip(names, before):
+        assert torch.equal(getattr(c.cache, x), y), x
+    c.check_read(lens)
