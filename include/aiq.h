@@ -642,11 +642,17 @@ aiq_status aiq_kv_attend_workspace_size(const aiq_kv_cache* cache, const aiq_kv_
  * with query head h reading K/V head h / (n_heads / n_kv_heads).  q: rows of
  * n_heads * head_dim elements of the cache's dtype, q_ld apart; out: the same
  * in out_dtype (AIQ_F16 or AIQ_BF16), out_ld apart; aligned as aiq_kv_write's
- * rows.  The row of an empty slot (len[i] = 0) becomes zero.  A query sees a
- * token only through the scale of its block: an infinity or NaN in the block
- * of a visible token reaches the output, one in later blocks does not.  With
- * one row per sequence at most (cu NULL, or n_rows no more than n_seq) the
- * result does not depend on the other sequences.
+ * rows.  The row of an empty slot (len[i] = 0) becomes zero.  Softmax weights
+ * are held in fp16 (for the tail of a bf16 cache in bf16) and their sums in
+ * fp32: before its own rounding the output is, within about 2^-11 (2^-8) of
+ * the largest |v| that the row sees, the formula's over what the cache holds,
+ * as long as its blocks' scales of values lie within 2^100 of each other (fp16's
+ * always do).  An infinity or NaN in the full block of a visible token, or
+ * among a visible tail token's values, makes the head's output infinite or NaN,
+ * in that dimension or in all; one in later blocks or of later tail tokens does
+ * not, and a query whose scores are all -infinity gives NaN.  With one row per
+ * sequence at most (cu NULL, or n_rows no more than n_seq) the result does not
+ * depend on the other sequences.
  * workspace: 256-byte aligned, aiq_kv_attend_workspace_size bytes (NULL where
  * that is 0); calls that may overlap need one each.  Errors: AIQ_EINVAL (as
  * aiq_kv_write; n_heads not a multiple of n_kv_heads), AIQ_EUNSUPPORTED (as

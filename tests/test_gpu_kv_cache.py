@@ -739,3 +739,22 @@ def test_rows_written_again(hd):
     for x, y in zip(names, before):
         assert torch.equal(getattr(c.cache, x), y), x
     c.check_read(lens)
+
+
+@pytest.mark.parametrize("new", [None, 5, 40])
+def test_values_of_blocks_scales_apart(new):
+    """Blocks of zeros (the least scale), of tiny and of large values, 2^96 apart: every one weighs what its scores say."""
+    say("case: scales of values apart", new)
+    n = 3 if new != 40 else 60
+    lens, ones = np.full(n, 150), np.full(n, new or 1)
+    c = Case(lens, 8, 2, 64, torch.bfloat16, 81)
+    for q, v in zip(c.q, c.v):
+        q *= 0.25
+        v[:32] = 0
+        v[32:64] *= 2.0 ** -70
+        v[64:96] *= 2.0 ** 16 / float(v[64:96].abs().max())
+    c.write(lens, lens)
+    out = c.cache.attend(c.batch(lens, ones, single=new is None), c.rows("q", lens, ones))
+    sel = np.zeros(n, np.int64)
+    sel[:3] = ones[:3]
+    c.check_attend(lens, sel, out[:3 * (new or 1)])
