@@ -574,11 +574,15 @@ hipError_t launch_kv_read(const KvCache& c, const KvBatch& b, const KvRows& r, h
 // += sum p' / v_scale: a block's scales cost two multiply-adds per score, the
 // bytes themselves (whole numbers, exact in fp16) go into the matrix products.
 // m follows the maximum only when that is more than 8 above it (so weights
-// stay below 2^8 and, with the fixed factor 2^7, in fp16's normal range down to 2^-29 of
-// the largest).  fp16 holds the weights to 2^-12, as the 16-bit attention does.
+// stay below 2^8 and, with the fixed factor 2^7, in fp16's normal range down to 2^-21 of
+// the largest at least).  fp16 holds the weights to 2^-11 relative, as the 16-bit attention does, and to 2^-25 below that
+// range (2^-32 of the largest); their sums stay in 32 bits.  The tail of a bf16 cache has bf16 values and a product
+// of that type: its weights are held to 2^-8 (the values may be past fp16's range).
 // Bound: HBM, as every byte of the cache is read once: 2,000 sequences of about 200 tokens (24/8 heads of 128, waves
 // alone) 224 us for 1.14 GB, 5.1 TB/s; 4 of 100,000 (32/8 heads of 64, split) 83 us for 417 MB, 5.0 TB/s; one of
-// 171 tokens 6.5 us, the chain of one wave's loads and products.
+// 171 tokens 6.5 us, the chain of one wave's loads and products; 256 of about 150 (8/8 heads of 64) 18 us for 52 MB, 2.8
+// TB/s: the four waves take up to 127 registers, so that four workgroups are on a CU, 1,024 of the 2,048 at a time, and long
+// sequences may start late.  These kernels keep 22 to 65 scalars in vector lanes; none of them spills to scratch.
 constexpr int KV_SEG = 16;       // blocks per segment
 constexpr float KV_SLACK = 8.0f, KV_UP = 7.0f;
 constexpr int KV_MANY = 48;      // rows per sequence from which on tiles of KV_ROWS take them
@@ -961,7 +965,7 @@ struct KvWave {
     } pf;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      pf.u[e] = BF ? f2bf(p[0][0][e]) : f2h(p[0][0][e]);
+      pf.u[e] = BF ? f2bf(p[0][0][e]) : f2h(p[0][0][e]);   // (rounded as the header of this part says)
       const int at = (e / 4) * 16 + g * 4 + e % 4;
       if (several && tok0 + at <= pos && bad[at]) l[0] = __uint_as_float(0x7FC00000u);   // (whatever it weighs: 0 times it is NaN)
     }
@@ -1240,9 +1244,11 @@ __global__ __launch_bounds__(256) void k_kv_join(KvAttendArgs a, int64_t n_tiles
 // become fp16 fragments once per workgroup, in LDS, in the order in which the products
 // take them (every access 16 bytes per lane, in lane order), the next two steps' bytes in
 // flight meanwhile.  Bound: the softmax's VALU work (16 scores per lane and block of
-// 32 keys, 8 exponentials of 4 issue slots each per tile) beside 32 matrix instructions, and the tail of the last
-// tiles.  64 sequences of about 900 tokens with 128 new ones, 24/8 heads of 128: 160 us, 650
-// TFLOP/s of products that are seen; 16 sequences of 4,000 with 512 830 TFLOP/s.
+// 32 keys, 8 exponentials of 4 issue slots each per tile) and 32 matrix instructions, by turns: two waves per SIMD overlap
+// little of them.  64 sequences of about 900 tokens with 128 new ones, 24/8 heads of 128: 155 us, 650
+// TFLOP/s of products that are seen, CUs busy 86% of the time, vector instructions in issue 45%, matrix units busy
+// 28%, LDS busy 25% (a fragment read feeds two products; no bank conflicts) and 3% of the waves' time spent waiting to issue
+// to it; 16 sequences of 4,000 with 512 830 TFLOP/s.
 constexpr int KV_ROWS = 128;
 constexpr int KV_LIST = 64;      // numbers and scales of twice as many blocks are in LDS
 constexpr int KV_AHEAD = 4;      // blocks whose bytes are in flight or staged
@@ -1585,6 +1591,8 @@ static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
   // against 56.  Where the tiles of 16 are few they run at once, four waves to a tile's keys: 16 sequences of 2,000 with
   // 16 (512 and 640 of them) 65 against 47 and 48 against 37, with 32 (896, 1,152) 67 against 81 and 52 against 57; 4 of
   // 4,000 with 64 (416, 544) 116 against 83 and 84 against 64, with 128 (800, 1,056) 121 against 137 and 87 against 93.
+  // (Between one row and those: 8 new rows of three heads are two tiles of 16, each reading all of the sequence's bytes, 66 us
+  // where the bytes take 38.)
   // (One row per sequence stays with the tiles of 16 whatever its heads: their order of sums is the keys' alone.)
   s.many = b.cu && b.n_rows > b.n_seq && b.n_rows * rep >= static_cast<int64_t>(b.n_seq) * KV_MANY &&
            s.tiles * c.n_kv >= 768;
@@ -1592,6 +1600,8 @@ static KvShape kv_shape(const KvCache& c, const KvBatch& b, int32_t n_heads) {
     s.tiles = big;
     return s;
   }
+  // Inside a query n_seq is the most sequences that a pass may hold, not how many the query selects (n_ptr): a selective
+  // one takes the rules' side for many.
   const int64_t items = s.tiles * c.n_kv;
   // Segments in workgroups of their own where (tile, K/V head) items leave CUs without work for long enough
   // to pay for the second launch (about 5 us).  Split against one workgroup per item, heads of 64: 8 items of

@@ -3,16 +3,23 @@
 // order of ids.
 //
 // A workgroup of 16 or 4 waves per row, each wave a run of ids; every pass reads the row again,
-// from the L2 where that still holds it (held in registers, 32 logits per thread, it left none for the passes
-// to overlap: 580 us for 4,096 rows of 32,000 against 465).
+// from the L2 where that still holds it.  (Held in registers, 32 logits per thread, a row per CU, the reading of 4,096 rows
+// of 32,000 did not overlap the arithmetic: 580 us against 465.  With no more rows than CUs, where there is nothing
+// to overlap, it has not been measured.)
 //
 // Bound: the vector unit, fp64 first of all (a weight is about 20 fp64 instructions), on the CUs that
-// have a row; one row after its latencies, a pass per 2 us or so.  Rows of 32,000 fp32 logits, us:
-//             temperature 0  no filter  top-k 50  top-k 1,000  top-p 0.9
-//   1 row            7          15         19          28          40
-//   256 rows         9          20         22          31          47
-//   2,048 rows      25         125         89         225         279   (262 MB: 55 us a reading, of two at least)
-// and 96 rows of 131,071 bf16 logits with top-k 1,000 and top-p 0.95 60, on 96 of the 256 CUs.
+// have a row; one row after its latencies, a pass per 2 us or so.  Rows of 32,000 fp32 logits in launches one after
+// another, us:
+//             temperature 0  no filter  min-p 0.05  top-k 50  top-k 1,000  top-k 2,000  top-p 0.9
+//   1 row            8          16         22          20         28          45           41
+//   256 rows         9          20         28          22         30          52           47
+//   2,048 rows      42         135        164          88        225         244          280
+//   the same cold   53         134        168         100        239         257          289
+// The rows of the first three lines (262 MB in the third) are those of the launch before, so what the 256 MB of
+// last-level cache keep of them is not read from HBM; "cold" are four such matrices in turn (55 us a reading).
+// 96 rows of 131,071 bf16 logits with top-k 1,000 and top-p 0.95 take 60, on 96 of the 256 CUs.
+// The 16-wave kernels with filters are at their 128 registers (16 waves on a CU) and spill 3 to 5 more to scratch (16 to 24
+// bytes per lane), as the 4-wave ones of fp32 do by 1 or 2.
 //
 // Weights are whole numbers, round(2^S exp((x - m) / T)) from fp64 exponentials
 // (below), S such that a whole vocabulary's sum fits 62 bits: sums do not
@@ -27,7 +34,10 @@
 // maximum (2,048 bins in LDS), the bin in which the count or the sum reaches its
 // target, and in that bin the token itself, by comparing its tokens (60 or so) with each other.
 // Where top-k leaves few tokens (draw_few) the steps after it are taken among those alone.
-// A bin with more than CAP tokens (equal logits, a far outlier) is halved bit by bit instead.
+// A bin with more than CAP tokens (equal logits, a far outlier) is halved bit by bit instead, 57 further passes over the
+// row: logits of four levels only, 32,000 of them, take 372 us with top-k and 696 with top-p where a row of the table
+// takes 20 and 41 (1,024 rows 1.5 and 2.9 ms), and 16-bit logits around 8 with 131,072 tokens, whose steps of 1/32 or 1/16
+// hold more than CAP tokens, 195 with top-p 0.9 (700 rows 738).
 #include "aiq_internal.h"
 #include "dev_util.h"
 
