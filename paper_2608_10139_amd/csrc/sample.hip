@@ -26,7 +26,8 @@
 // depend on their order, so they may come from LDS atomics, and a weight keeps
 // 2^-47 of the largest at 32,000 tokens.  (In 32 bits a border between two tokens
 // moves by 1e-7 of the sum, which is a share of 3e-3 of all random numbers with
-// 32,000 borders; here it is below 1e-8.)
+// 32,000 borders.  Here it moves by less than V^2 2^-61: V roundings of half a step, in the sum up to it and in the whole,
+// which is 2^S >= 2^61 / V at least.)
 //
 // All filters keep a prefix of the tokens in descending order, equal ones by
 // ascending id, so the kept set is a threshold (x, id).  Top-k and top-p find theirs
