@@ -681,8 +681,8 @@ aiq_status aiq_kv_attend(const aiq_kv_cache* cache, const aiq_kv_batch* batch, c
  * where the maximum is +infinity, its tokens weigh 1 and the others nothing.
  * Weights are taken from fp64 exponentials and summed as whole numbers, so
  * results do not depend on an order of summation; a border between two tokens
- * is off by less than vocab^2 2^-61 of the unit interval (4e-10 at 32,000
- * tokens, 8e-9 at 131,072, but 2^-13 at 2^24).
+ * (u's, and that of n_p) is off by less than vocab^2 2^-61 of the sum (4e-10 at
+ * 32,000 tokens, 8e-9 at 131,072, but 2^-13 at 2^24).
  * vocab at most 2^24, ld >= vocab or 0.  Errors: AIQ_EINVAL (NULL pointer,
  * negative count or top_k, temperature negative or not finite, top_p
  * outside (0, 1], min_p outside [0, 1], logits not aligned to their type),
